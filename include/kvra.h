@@ -389,6 +389,74 @@ int kvra_layer_chunk(const kvra_layer* layer, const void* x, void* y, void* k_ca
                      int64_t prefix_len, int64_t chunk_len, int64_t capacity,
                      void* workspace, int64_t workspace_bytes, void* stream);
 
+/*
+ * ---- The cache in 8 bits, the weights in 4 --------------------------------------------------------
+ * Behind the prompt a token's step reads the cache and the weights once and computes little: its time is their
+ * bytes.  These calls are the ones above with both held small.  Both formats are small floating point
+ * values with a power-of-two scale for each block (e8m0: one byte, the scale is 2^(byte - 127)):
+ *   cache    e4m3 (OCP, no infinities; 0x7F and 0xFF are NaN), a scale for each block of 64 consecutive tokens
+ *            (rows 64 b .. 64 b + 63) and head, separate ones for K and V;
+ *   weights  e2m1 (0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives), two to a byte, the first of a pair in the low
+ *            four bits, a scale for each 32 consecutive values of a row.
+ * A block's exponent e is the smallest with which its largest finite magnitude does not overflow (<= 448 * 2^e,
+ * <= 6 * 2^e), kept within -100 .. 120; values are rounded to nearest, ties to even.  A value of either format
+ * times its scale is an exact bf16 number (e4m3: up to 248 * 2^120): the calls compute with those.
+ * Tensors other than scales are 16-byte aligned (KVRA_EINVAL otherwise).
+ */
+
+/*
+ * kvra_append_kv into an 8-bit cache.  K is rotated in fp64, so that the one rounding is that to e4m3.
+ *   k_in, v_in  as kvra_append_kv (device, read)
+ *   q_in, q_out [chunk_len, n_q_heads, head_dim] bf16, both or neither NULL; q_out = rotated q_in, the same bits
+ *           kvra_append_kv leaves; may be the same tensor
+ *   k_cache, v_cache [capacity, n_kv_heads, head_dim] bytes; k_scale, v_scale [ceil(capacity / 64), n_kv_heads] bytes
+ * Rows [prefix_len, prefix_len + chunk_len) are written and the scales of their blocks.  Nothing else is, with one
+ * exception: where the chunk starts inside a block, the scale found there (that of an earlier append; rows
+ * of the block ahead of prefix_len are taken to be valid) never shrinks, and if a new value asks for a larger one, the
+ * block's earlier rows are rescaled, which is exact for all but values below the smallest normal number of
+ * the new scale.  A cache needs no initialisation.
+ * A NaN or an infinity is stored as NaN and does not count towards the scale.
+ * Errors: KVRA_EINVAL, KVRA_EUNSUPPORTED, KVRA_ERANGE, KVRA_ELAUNCH, as kvra_append_kv.
+ */
+int kvra_append_kv_q8(const void* k_in, const void* v_in, const void* q_in, void* q_out,
+                      void* k_cache, void* v_cache, void* k_scale, void* v_scale,
+                      int64_t prefix_len, int64_t chunk_len, int64_t capacity,
+                      int n_q_heads, int n_kv_heads, int head_dim, float rope_base, void* stream);
+
+/*
+ * kvra_chunk_attn over an 8-bit cache, from one token (a step behind the prompt) to a whole chunk.
+ *   q, scale, out   as kvra_chunk_attn; k_cache .. v_scale as kvra_append_kv_q8 leaves them, rows
+ *               [0, prefix_len + chunk_len) valid (others are not read, whatever they hold)
+ *   workspace   caller-owned device memory, 256-byte aligned, at least kvra_chunk_attn_q8_workspace_bytes() (100 MiB,
+ *               enough for every shape).  Its first 16 KiB have to be zero before its first use, and every call leaves them
+ *               zero; the rest is scratch.  Calls that may overlap in time (other streams, graphs replayed side
+ *               by side) need a workspace each.
+ * The library allocates nothing and keeps nothing: a call may be captured into a graph as it is.
+ * A NaN in a row of K that a query sees makes its result NaN; one in a row of V at least the component that holds it.  What a query
+ * does not see does not reach it, NaN included.
+ * Errors: KVRA_EINVAL (also: workspace short or misaligned), KVRA_EUNSUPPORTED, KVRA_ELAUNCH, KVRA_ENODEVICE.
+ */
+int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,
+                       int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim,
+                       float scale, void* out, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t kvra_chunk_attn_q8_workspace_bytes(void);
+
+/*
+ * Weights into the 4-bit format and back.  w [n, k] bf16; codes [n, k / 2] bytes; scales [n, k / 32] bytes.  n must be a multiple of 32 and
+ * k of 64, and w must stay below 4 GiB (KVRA_EUNSUPPORTED).  A group of 32 that holds an infinity or a NaN
+ * becomes NaN as a whole (scale byte 255), which kvra_unpack_w4 and kvra_linear_w4 give back.
+ */
+int kvra_pack_w4(const void* w, void* codes, void* scales, int64_t n, int64_t k, void* stream);
+int kvra_unpack_w4(const void* codes, const void* scales, void* w, int64_t n, int64_t k, void* stream);
+
+/*
+ * kvra_linear with 4-bit weights, for one token as for a prompt: the same products and epilogues as
+ * kvra_linear on what kvra_unpack_w4 gives, fp32 accumulation (the order of sums may differ).  w2 and w2_scale
+ * are both given (SwiGLU) or both NULL.  m is free; n, k and the sizes of x and of the unpacked w are bound as there.
+ */
+int kvra_linear_w4(const void* x, const void* w, const void* w_scale, const void* w2, const void* w2_scale,
+                   const void* residual, void* out, int64_t m, int64_t n, int64_t k, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -289,3 +289,79 @@ extern "C" int kvra_layer_chunk(const kvra_layer* L, const void* x, void* y, voi
     return rc;
   return kvra::launch_linear(act, L->w_down, nullptr, x2, &y, hidden_cols, 1, c, L->hidden, L->ffn, st, shared);
 }
+
+// ---------------------------------------------------------------- the cache in 8 bits, the weights in 4
+namespace {
+
+bool aligned(const void* p, unsigned to = 16) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+}  // namespace
+
+extern "C" int kvra_append_kv_q8(const void* k_in, const void* v_in, const void* q_in, void* q_out,
+                                 void* k_cache, void* v_cache, void* k_scale, void* v_scale,
+                                 int64_t prefix_len, int64_t chunk_len, int64_t capacity,
+                                 int n_q_heads, int n_kv_heads, int head_dim, float rope_base, void* stream) {
+  if (k_in == nullptr || v_in == nullptr || k_cache == nullptr || v_cache == nullptr || k_scale == nullptr || v_scale == nullptr)
+    return KVRA_EINVAL;
+  if ((q_in == nullptr) != (q_out == nullptr)) return KVRA_EINVAL;
+  if (chunk_len < 1 || prefix_len < 0 || capacity < 1) return KVRA_EINVAL;
+  if (!(rope_base == rope_base)) return KVRA_EINVAL;
+  int rc = check_heads(n_q_heads, n_kv_heads, head_dim);
+  if (rc != KVRA_OK) return rc;
+  if (!aligned(k_in) || !aligned(v_in) || !aligned(q_in) || !aligned(q_out) || !aligned(k_cache) || !aligned(v_cache)) return KVRA_EINVAL;
+  if (chunk_len > kMaxTokens || prefix_len > kMaxTokens) return KVRA_EUNSUPPORTED;
+  if (prefix_len + chunk_len > capacity) return KVRA_ERANGE;
+  return kvra::launch_append_kv_q8(k_in, v_in, q_in, q_out, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len,
+                                   n_q_heads, n_kv_heads, head_dim, rope_base, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int64_t kvra_chunk_attn_q8_workspace_bytes(void) { return kvra::attn_q8_workspace_bytes(); }
+
+extern "C" int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,
+                                  int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim,
+                                  float scale, void* out, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (q == nullptr || k_cache == nullptr || v_cache == nullptr || k_scale == nullptr || v_scale == nullptr || out == nullptr ||
+      workspace == nullptr)
+    return KVRA_EINVAL;
+  if (chunk_len < 1 || prefix_len < 0) return KVRA_EINVAL;
+  if (!(scale > 0.0f) || !(scale < INFINITY)) return KVRA_EINVAL;
+  int rc = check_heads(n_q_heads, n_kv_heads, head_dim);
+  if (rc != KVRA_OK) return rc;
+  if (!aligned(q) || !aligned(k_cache) || !aligned(v_cache) || !aligned(out)) return KVRA_EINVAL;
+  if (workspace_bytes < kvra::attn_q8_workspace_bytes() || !aligned(workspace, 256)) return KVRA_EINVAL;
+  if (chunk_len > kMaxTokens || prefix_len > kMaxTokens) return KVRA_EUNSUPPORTED;
+  return kvra::launch_chunk_attn_q8(kvra::Q8Cache{k_cache, v_cache, k_scale, v_scale}, q, prefix_len, chunk_len, n_q_heads,
+                                    n_kv_heads, head_dim, scale, out, workspace, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+
+int check_w4(int64_t n, int64_t k) {
+  if (n < 1 || k < 1) return KVRA_EINVAL;
+  if (n % 32 != 0 || k % 64 != 0 || n > (int64_t(1) << 24) || n * k * 2 >= kMaxOperandBytes) return KVRA_EUNSUPPORTED;
+  return KVRA_OK;
+}
+
+}  // namespace
+
+extern "C" int kvra_pack_w4(const void* w, void* codes, void* scales, int64_t n, int64_t k, void* stream) {
+  if (w == nullptr || codes == nullptr || scales == nullptr || !aligned(w) || !aligned(codes)) return KVRA_EINVAL;
+  const int rc = check_w4(n, k);
+  return rc != KVRA_OK ? rc : kvra::launch_pack_w4(w, codes, scales, n, k, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int kvra_unpack_w4(const void* codes, const void* scales, void* w, int64_t n, int64_t k, void* stream) {
+  if (w == nullptr || codes == nullptr || scales == nullptr || !aligned(w) || !aligned(codes)) return KVRA_EINVAL;
+  const int rc = check_w4(n, k);
+  return rc != KVRA_OK ? rc : kvra::launch_unpack_w4(codes, scales, w, n, k, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int kvra_linear_w4(const void* x, const void* w, const void* w_scale, const void* w2, const void* w2_scale,
+                              const void* residual, void* out, int64_t m, int64_t n, int64_t k, void* stream) {
+  if (x == nullptr || w == nullptr || w_scale == nullptr || out == nullptr) return KVRA_EINVAL;
+  if ((w2 == nullptr) != (w2_scale == nullptr) || (w2 != nullptr && residual != nullptr)) return KVRA_EINVAL;
+  if (!aligned(x) || !aligned(w) || !aligned(w2) || !aligned(residual) || !aligned(out)) return KVRA_EINVAL;
+  int rc = check_linear(m, n, k);
+  if (rc != KVRA_OK) return rc;
+  return kvra::launch_linear_w4(x, w, w_scale, w2, w2_scale, residual, out, m, n, k, static_cast<hipStream_t>(stream));
+}

@@ -867,6 +867,17 @@ int device_cus(int dev) {
   return g_cus[dev];
 }
 
+}  // namespace
+
+int current_device_cus() {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+  std::lock_guard<std::mutex> lock(g_scratch_mutex);
+  return device_cus(dev);
+}
+
+namespace {
+
 // The allocated scratch of the current device, or nullptr (the caller then launches without cutting
 // units).  A failed attempt is not remembered: a call made while `stream` is being captured (an
 // allocation would be illegal there) or while memory is short runs uncut, and a later call tries again.

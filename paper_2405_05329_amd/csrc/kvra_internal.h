@@ -122,6 +122,33 @@ int launch_rms_norm_angles(const void* x, const void* gain, void* y, int64_t row
                            int head_dim, float rope_base, float* angles, hipStream_t stream);
 int rms_norm_max_hidden();
 
+// ---- the cache in 8 bits, the weights in 4 --------------------------------------------------------------------------
+int launch_append_kv_q8(const void* k_in, const void* v_in, const void* q_in, void* q_out, void* k_cache, void* v_cache,
+                        void* k_scale, void* v_scale, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
+                        int head_dim, float rope_base, hipStream_t stream);
+
+struct Q8Cache {
+  const void* k;
+  const void* v;
+  const void* k_scale;
+  const void* v_scale;
+};
+// Slices of `rows` (16 or 32) virtual rows, `splits` workgroups each; splits > 1 needs attn_rows_q8_slot_bytes(head_dim, rows)
+// for every workgroup and, zero between launches, a counter per slice.
+int launch_attn_rows_q8(const Q8Cache& cache, const void* q, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
+                        int head_dim, float scale, void* out, int rows, int splits, float* partial, int* counters,
+                        hipStream_t stream);
+int64_t attn_rows_q8_slot_bytes(int head_dim, int rows);
+int64_t attn_q8_workspace_bytes();
+int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
+                         int head_dim, float scale, void* out, void* workspace, hipStream_t stream);
+int current_device_cus();   // 0 if it cannot be asked
+
+int launch_pack_w4(const void* w, void* codes, void* scales, int64_t n, int64_t k, hipStream_t stream);
+int launch_unpack_w4(const void* codes, const void* scales, void* w, int64_t n, int64_t k, hipStream_t stream);
+int launch_linear_w4(const void* x, const void* w, const void* ws, const void* w2, const void* ws2, const void* residual, void* out,
+                     int64_t m, int64_t n, int64_t k, hipStream_t stream);
+
 // More than 64 KiB of dynamic LDS has to be granted per kernel and device.  A thread remembers what it has asked for (the
 // request goes through the runtime's locks: 0.3 of a 3.5 us call).
 inline bool grant_lds(const void* kernel, unsigned bytes) {

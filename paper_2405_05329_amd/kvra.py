@@ -108,6 +108,18 @@ def _load() -> ctypes.CDLL:
     lib.kvra_layer_workspace_bytes.argtypes = [ctypes.POINTER(KvraLayer), i64]
     lib.kvra_layer_chunk.restype = i32
     lib.kvra_layer_chunk.argtypes = [ctypes.POINTER(KvraLayer), vp, vp, vp, vp, i64, i64, i64, vp, i64, vp]
+    lib.kvra_append_kv_q8.restype = i32
+    lib.kvra_append_kv_q8.argtypes = [vp] * 8 + [i64, i64, i64, i32, i32, i32, f32, vp]
+    lib.kvra_chunk_attn_q8.restype = i32
+    lib.kvra_chunk_attn_q8.argtypes = [vp] * 5 + [i64, i64, i32, i32, i32, f32, vp, vp, i64, vp]
+    lib.kvra_chunk_attn_q8_workspace_bytes.restype = i64
+    lib.kvra_chunk_attn_q8_workspace_bytes.argtypes = []
+    lib.kvra_pack_w4.restype = i32
+    lib.kvra_pack_w4.argtypes = [vp, vp, vp, i64, i64, vp]
+    lib.kvra_unpack_w4.restype = i32
+    lib.kvra_unpack_w4.argtypes = [vp, vp, vp, i64, i64, vp]
+    lib.kvra_linear_w4.restype = i32
+    lib.kvra_linear_w4.argtypes = [vp] * 7 + [i64, i64, i64, vp]
     return lib
 
 
@@ -463,3 +475,46 @@ def kvra_layer_chunk(layer: KvraLayer, x, y, k_cache, v_cache, prefix_len, chunk
                            workspace_bytes, stream)
     if rc != KVRA_OK:
         raise KvraError(rc, "kvra_layer_chunk")
+
+
+def kvra_append_kv_q8(k_in, v_in, q_in, q_out, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len, capacity,
+                      n_q_heads, n_kv_heads, head_dim, rope_base, stream=None, check=True) -> int:
+    rc = _lib.kvra_append_kv_q8(_ptr(k_in), _ptr(v_in), _ptr(q_in), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                                _ptr(v_scale), int(prefix_len), int(chunk_len), int(capacity), int(n_q_heads), int(n_kv_heads),
+                                int(head_dim), float(rope_base), _stream(stream))
+    if check and rc != KVRA_OK:
+        raise KvraError(rc, "kvra_append_kv_q8")
+    return rc
+
+
+def kvra_chunk_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim,
+                       scale, out, workspace, workspace_bytes, stream=None, check=True) -> int:
+    rc = _lib.kvra_chunk_attn_q8(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), int(prefix_len),
+                                 int(chunk_len), int(n_q_heads), int(n_kv_heads), int(head_dim), float(scale), _ptr(out),
+                                 _ptr(workspace), int(workspace_bytes), _stream(stream))
+    if check and rc != KVRA_OK:
+        raise KvraError(rc, "kvra_chunk_attn_q8")
+    return rc
+
+
+def kvra_chunk_attn_q8_workspace_bytes() -> int:
+    return int(_lib.kvra_chunk_attn_q8_workspace_bytes())
+
+
+def kvra_pack_w4(w, codes, scales, n, k, stream=None):
+    rc = _lib.kvra_pack_w4(_ptr(w), _ptr(codes), _ptr(scales), int(n), int(k), _stream(stream))
+    if rc != KVRA_OK:
+        raise KvraError(rc, "kvra_pack_w4")
+
+
+def kvra_unpack_w4(codes, scales, w, n, k, stream=None):
+    rc = _lib.kvra_unpack_w4(_ptr(codes), _ptr(scales), _ptr(w), int(n), int(k), _stream(stream))
+    if rc != KVRA_OK:
+        raise KvraError(rc, "kvra_unpack_w4")
+
+
+def kvra_linear_w4(x, w, w_scale, w2, w2_scale, residual, out, m, n, k, stream=None):
+    rc = _lib.kvra_linear_w4(_ptr(x), _ptr(w), _ptr(w_scale), _ptr(w2), _ptr(w2_scale), _ptr(residual), _ptr(out), int(m), int(n),
+                             int(k), _stream(stream))
+    if rc != KVRA_OK:
+        raise KvraError(rc, "kvra_linear_w4")

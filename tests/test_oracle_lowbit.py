@@ -1,0 +1,152 @@
+"""Pins of the oracle of the 8-bit cache and the 4-bit weights: the formats' tables against torch's conversions and hand-worked
+values, scale borders, ties, growth of a block's scale, and attention and linear layers against the pinned bf16 oracle.  And the
+refusals of the entry points, which need no GPU."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kvra_oracle as orc
+from oracle import lowbit
+from paper_2405_05329_amd import kvra
+
+
+def test_e4m3_is_torchs():
+    codes = np.arange(256, dtype=np.uint8)
+    want = torch.from_numpy(codes).view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(lowbit.e4m3_values(codes), want, equal_nan=True)
+    x = np.concatenate([want[np.isfinite(want)] * f for f in (1.0, 1.03125, 1.0625, 0.97)])
+    x = x[np.abs(x) <= 448]
+    got = lowbit.e4m3_codes(x, 0)
+    assert np.array_equal(got, torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy())
+    assert list(lowbit.e4m3_codes(np.array([np.inf, -np.inf, 464.0 - 17]), 0)) == [127, 255, 126]
+
+
+def test_e2m1_values_and_ties():
+    assert list(lowbit.E2M1) == [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+    x = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 0.2500001, -5.0000001, 9.0])
+    assert list(lowbit.nearest(x, lowbit.E2M1)) == [0, 2, 2, 4, 4, 6, 6, 1, 15, 7]
+
+
+@pytest.mark.parametrize("most", [448.0, 6.0])
+def test_the_smallest_scale_that_holds_the_peak(most):
+    for e in (-90, -3, 0, 5, 100):
+        border = most * 2.0 ** e
+        assert list(lowbit.exponent([border, border * (1 + 1e-15), border * (1 - 1e-15)], most)) == [e, e + 1, e]
+        assert lowbit.exponent(border / 2, most) == e - 1
+    assert list(lowbit.exponent([0.0, 1e-300, 1e300], most)) == [-100, -100, 120]
+
+
+def test_a_blocks_scale_grows_and_its_rows_follow():
+    cache, scale = np.full((70, 1, 64), 0x7F, np.uint8), np.full((2, 1), 9, np.uint8)
+    small, large = np.full((3, 1, 64), 1.125), np.full((2, 1, 64), 1.75 * 2.0 ** 9)
+    lowbit.append_rows(cache, scale, small, 0)
+    assert scale[0, 0] == 127 - 8 and np.all(lowbit.cache_values(cache, scale)[:3] == 1.125)
+    lowbit.append_rows(cache, scale, large, 3)
+    assert scale[0, 0] == 128 and np.all(lowbit.cache_values(cache, scale)[:5] == np.concatenate([small, large]))
+    lowbit.append_rows(cache, scale, small[:1], 5)
+    assert scale[0, 0] == 128 and lowbit.cache_values(cache, scale)[5, 0, 0] == 1.125
+    assert np.all(cache[6:] == 0x7F) and scale[1, 0] == 9
+    tiny = np.full((1, 1, 64), 2.0 ** -9)
+    tiny[..., 1] = np.nan
+    lowbit.append_rows(cache, scale, tiny, 64)
+    assert scale[1, 0] == 127 - 17 and np.isnan(lowbit.cache_values(cache, scale)[64, 0, 1])
+
+
+def test_pack_and_unpack():
+    rng = np.random.default_rng(5)
+    w = rng.standard_normal((32, 128))
+    w[0, :32], w[1, 5], w[2, 40] = 0.0, np.inf, np.nan
+    codes, scales = lowbit.pack(w)
+    v = lowbit.unpack(codes, scales)
+    assert codes.shape == (32, 64) and scales.shape == (32, 4)
+    assert np.isnan(v[1, :32]).all() and np.isnan(v[2, 32:64]).all() and np.isfinite(v[3:]).all() and np.all(v[0, :32] == 0)
+    peak = np.abs(w[3:].reshape(29, 4, 32)).max(axis=2)
+    assert np.all(np.abs(w[3:] - v[3:]).reshape(29, 4, 32).max(axis=2) <= peak / 3)      # half of the widest gap (4 to 6) over 3: peak > 3 * 2^e
+    again = lowbit.pack(v[3:])
+    assert np.array_equal(lowbit.unpack(*again), v[3:])
+
+
+def test_attention_and_linear_are_the_pinned_oracles():
+    rng = np.random.default_rng(6)
+    q, k, v = rng.standard_normal((5, 4, 64)), rng.standard_normal((9, 2, 64)), rng.standard_normal((9, 2, 64))
+    out, mass, reach = lowbit.attention(q, k, v, 4, 0.3)
+    assert np.allclose(out, orc.chunk_attention(q, k, v, 4, 5, 0.3), rtol=0, atol=1e-13)
+    assert np.all(mass >= np.abs(out) - 1e-13) and reach.shape == (5, 4, 1)
+    codes, scales = lowbit.pack(rng.standard_normal((32, 64)))
+    codes2, scales2 = lowbit.pack(rng.standard_normal((32, 64)))
+    x = rng.standard_normal((3, 64))
+    w, w2 = lowbit.unpack(codes, scales), lowbit.unpack(codes2, scales2)
+    assert np.allclose(lowbit.linear(x, codes, scales)[0], orc.linear(x, w), atol=1e-13)
+    assert np.allclose(lowbit.linear(x, codes, scales, codes2, scales2)[0], orc.silu(x @ w.T) * (x @ w2.T), atol=1e-13)
+
+
+# ---- refusals ----------------------------------------------------------------------------------------------------------
+A = [4096 * (i + 1) for i in range(8)]
+INVALID, UNSUPPORTED, RANGE = kvra.KVRA_EINVAL, kvra.KVRA_EUNSUPPORTED, kvra.KVRA_ERANGE
+
+
+def _append(*, p=0, c=1, cap=64, H=2, Hkv=2, d=64, base=1e4, **other):
+    t = dict(zip(("k_in", "v_in", "q_in", "q_out", "k_cache", "v_cache", "k_scale", "v_scale"), A), **other)
+    return kvra.kvra_append_kv_q8(*t.values(), p, c, cap, H, Hkv, d, base, check=False)
+
+
+def _attn(*, p=0, c=1, H=2, Hkv=2, d=64, scale=0.1, bytes_=None, **other):
+    t = dict(zip(("q", "k_cache", "v_cache", "k_scale", "v_scale", "out", "workspace"), A), **other)
+    return kvra.kvra_chunk_attn_q8(*list(t.values())[:5], p, c, H, Hkv, d, scale, t["out"], t["workspace"],
+                                   kvra.kvra_chunk_attn_q8_workspace_bytes() if bytes_ is None else bytes_, check=False)
+
+
+@pytest.mark.parametrize("want,args", [
+    *((INVALID, {name: None}) for name in ("k_in", "v_in", "q_in", "q_out", "k_cache", "v_cache", "k_scale", "v_scale")),
+    *((INVALID, {name: 4104}) for name in ("k_in", "v_in", "q_in", "q_out", "k_cache", "v_cache")),
+    (INVALID, dict(c=0)), (INVALID, dict(p=-1)), (INVALID, dict(cap=0)), (INVALID, dict(base=math.nan)), (INVALID, dict(H=3)),
+    (INVALID, dict(Hkv=0)), (UNSUPPORTED, dict(d=96)), (UNSUPPORTED, dict(H=1026)), (UNSUPPORTED, dict(c=(1 << 24) + 1, cap=1 << 30)),
+    (RANGE, dict(p=63, c=2)),
+])
+def test_append_refusals(want, args):
+    assert _append(**args) == want
+
+
+@pytest.mark.parametrize("want,args", [
+    *((INVALID, {name: None}) for name in ("q", "k_cache", "v_cache", "k_scale", "v_scale", "out", "workspace")),
+    *((INVALID, {name: 4104}) for name in ("q", "k_cache", "v_cache", "out", "workspace")),
+    (INVALID, dict(workspace=4096 + 16)), (INVALID, dict(bytes_=1 << 20)), (INVALID, dict(c=0)), (INVALID, dict(p=-1)),
+    (INVALID, dict(scale=0.0)), (INVALID, dict(scale=-1.0)), (INVALID, dict(scale=math.inf)), (INVALID, dict(scale=math.nan)),
+    (INVALID, dict(H=3)), (UNSUPPORTED, dict(d=32)), (UNSUPPORTED, dict(p=(1 << 24) + 1)),
+    (UNSUPPORTED, dict(c=1 << 24, H=128, Hkv=1)),
+])
+def test_attention_refusals(want, args):
+    assert _attn(**args) == want
+
+
+def _code(call, *args):
+    with pytest.raises(kvra.KvraError) as e:
+        call(*args)
+    return e.value.code
+
+
+def test_weight_refusals():
+    a = A
+    for call in (kvra.kvra_pack_w4, kvra.kvra_unpack_w4):
+        for i in range(3):
+            assert _code(call, *(None if j == i else a[j] for j in range(3)), 32, 64) == INVALID
+        assert _code(call, 4104, a[1], 4104, 32, 64) == INVALID
+        assert _code(call, a[0], a[1], a[2], 0, 64) == INVALID
+        assert _code(call, a[0], a[1], a[2], 33, 64) == _code(call, a[0], a[1], a[2], 32, 96) == UNSUPPORTED
+        assert _code(call, a[0], a[1], a[2], 1 << 20, 1 << 12) == UNSUPPORTED
+    lin = lambda x=a[0], w=a[1], s=a[2], w2=None, s2=None, r=None, o=a[3], m=1, n=32, k=64: _code(kvra.kvra_linear_w4, x, w, s, w2, s2, r, o, m, n, k)
+    assert lin(x=None) == lin(w=None) == lin(s=None) == lin(o=None) == lin(w2=a[4]) == lin(s2=a[4]) == INVALID
+    assert lin(w2=a[4], s2=a[5], r=a[6]) == lin(x=4104) == lin(w=4104) == lin(r=4104) == lin(o=4104) == lin(m=0) == INVALID
+    assert lin(n=48) == lin(k=32) == lin(m=1 << 20, k=1 << 12) == lin(m=(1 << 24) + 1) == UNSUPPORTED
+
+
+def test_tensors_that_may_not_be_passed():
+    t = torch.zeros(64, 64)
+    with pytest.raises(ValueError):
+        _append(k_in=t)
+    with pytest.raises(ValueError):
+        _attn(workspace=t.t())
+    with pytest.raises(ValueError):
+        kvra.kvra_linear_w4(t, A[0], A[1], None, None, None, A[2], 1, 32, 64)
