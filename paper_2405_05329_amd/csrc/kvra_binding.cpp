@@ -27,6 +27,11 @@ struct Entry {
   decltype(&kvra_linear) linear;
   decltype(&kvra_qkv_proj) qkv_proj;
   decltype(&kvra_layer_chunk) layer_chunk;
+  decltype(&kvra_append_kv_q8) append_kv_q8;
+  decltype(&kvra_chunk_attn_q8) chunk_attn_q8;
+  decltype(&kvra_pack_w4) pack_w4;
+  decltype(&kvra_unpack_w4) unpack_w4;
+  decltype(&kvra_linear_w4) linear_w4;
 } g_entry = {};
 
 // One call's arguments, in order; the first failure sticks and leaves a Python exception set.
@@ -190,14 +195,62 @@ PyObject* layer_chunk(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return call(r, [&] { return g_entry.layer_chunk(layer, x, y, kc, vc, prefix, chunk, capacity, ws, bytes, st); });
 }
 
-// bind(ptr_fallback, append_kv, chunk_attn, rms_norm, linear, qkv_proj, layer_chunk): the addresses of the entry points
+PyObject* append_kv_q8(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Reader r(args, n, 16);
+  void *k = r.pointer(), *v = r.pointer(), *q = r.pointer(), *qo = r.pointer(), *kc = r.pointer(), *vc = r.pointer();
+  void *ks = r.pointer(), *vs = r.pointer();
+  const int64_t prefix = r.integer(), chunk = r.integer(), capacity = r.integer();
+  const int H = r.small(), Hkv = r.small(), d = r.small();
+  const float base = r.real();
+  void* const st = r.stream();
+  return call(r, [&] { return g_entry.append_kv_q8(k, v, q, qo, kc, vc, ks, vs, prefix, chunk, capacity, H, Hkv, d, base, st); });
+}
+
+PyObject* chunk_attn_q8(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Reader r(args, n, 15);
+  void *q = r.pointer(), *kc = r.pointer(), *vc = r.pointer(), *ks = r.pointer(), *vs = r.pointer();
+  const int64_t prefix = r.integer(), chunk = r.integer();
+  const int H = r.small(), Hkv = r.small(), d = r.small();
+  const float scale = r.real();
+  void *out = r.pointer(), *ws = r.pointer();
+  const int64_t bytes = r.integer();
+  void* const st = r.stream();
+  return call(r, [&] { return g_entry.chunk_attn_q8(q, kc, vc, ks, vs, prefix, chunk, H, Hkv, d, scale, out, ws, bytes, st); });
+}
+
+PyObject* pack_w4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Reader r(args, n, 6);
+  void *w = r.pointer(), *codes = r.pointer(), *scales = r.pointer();
+  const int64_t rows = r.integer(), k = r.integer();
+  void* const st = r.stream();
+  return call(r, [&] { return g_entry.pack_w4(w, codes, scales, rows, k, st); });
+}
+
+PyObject* unpack_w4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Reader r(args, n, 6);
+  void *codes = r.pointer(), *scales = r.pointer(), *w = r.pointer();
+  const int64_t rows = r.integer(), k = r.integer();
+  void* const st = r.stream();
+  return call(r, [&] { return g_entry.unpack_w4(codes, scales, w, rows, k, st); });
+}
+
+PyObject* linear_w4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Reader r(args, n, 11);
+  void *x = r.pointer(), *w = r.pointer(), *ws = r.pointer(), *w2 = r.pointer(), *ws2 = r.pointer(), *res = r.pointer(), *out = r.pointer();
+  const int64_t m = r.integer(), cols = r.integer(), k = r.integer();
+  void* const st = r.stream();
+  return call(r, [&] { return g_entry.linear_w4(x, w, ws, w2, ws2, res, out, m, cols, k, st); });
+}
+
+// bind(ptr_fallback, append_kv, chunk_attn, rms_norm, linear, qkv_proj, layer_chunk, append_kv_q8, chunk_attn_q8, pack_w4, unpack_w4,
+// linear_w4): the addresses of the entry points
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 7 || !PyCallable_Check(args[0])) {
-    PyErr_SetString(PyExc_TypeError, "bind(callable, six addresses)");
+  if (n != 12 || !PyCallable_Check(args[0])) {
+    PyErr_SetString(PyExc_TypeError, "bind(callable, eleven addresses)");
     return nullptr;
   }
-  void* f[6];
-  for (int i = 0; i < 6; ++i) {
+  void* f[11];
+  for (int i = 0; i < 11; ++i) {
     f[i] = PyLong_AsVoidPtr(args[i + 1]);
     if (f[i] == nullptr) {
       if (PyErr_Occurred() == nullptr) PyErr_SetString(PyExc_ValueError, "an entry point is missing");
@@ -210,6 +263,11 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   g_entry.linear = reinterpret_cast<decltype(&kvra_linear)>(f[3]);
   g_entry.qkv_proj = reinterpret_cast<decltype(&kvra_qkv_proj)>(f[4]);
   g_entry.layer_chunk = reinterpret_cast<decltype(&kvra_layer_chunk)>(f[5]);
+  g_entry.append_kv_q8 = reinterpret_cast<decltype(&kvra_append_kv_q8)>(f[6]);
+  g_entry.chunk_attn_q8 = reinterpret_cast<decltype(&kvra_chunk_attn_q8)>(f[7]);
+  g_entry.pack_w4 = reinterpret_cast<decltype(&kvra_pack_w4)>(f[8]);
+  g_entry.unpack_w4 = reinterpret_cast<decltype(&kvra_unpack_w4)>(f[9]);
+  g_entry.linear_w4 = reinterpret_cast<decltype(&kvra_linear_w4)>(f[10]);
   Py_INCREF(args[0]);
   Py_XSETREF(g_ptr_fallback, args[0]);
   Py_RETURN_NONE;
@@ -217,7 +275,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define KVRA_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {KVRA_METHOD(bind),   KVRA_METHOD(append_kv), KVRA_METHOD(chunk_attn),  KVRA_METHOD(rms_norm),
-                           KVRA_METHOD(linear), KVRA_METHOD(qkv_proj),  KVRA_METHOD(layer_chunk), {nullptr, nullptr, 0, nullptr}};
+                           KVRA_METHOD(linear), KVRA_METHOD(qkv_proj),  KVRA_METHOD(layer_chunk), KVRA_METHOD(append_kv_q8), KVRA_METHOD(chunk_attn_q8), KVRA_METHOD(pack_w4),
+                           KVRA_METHOD(unpack_w4), KVRA_METHOD(linear_w4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_kvra_call", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -191,6 +191,33 @@ class _CtypesCalls:
                                      int(prefix_len), int(chunk_len), int(capacity), _ptr(workspace), int(workspace_bytes),
                                      _stream(stream))
 
+    @staticmethod
+    def append_kv_q8(k_in, v_in, q_in, q_out, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len, capacity, n_q_heads,
+                     n_kv_heads, head_dim, rope_base, stream):
+        return _lib.kvra_append_kv_q8(_ptr(k_in), _ptr(v_in), _ptr(q_in), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                                      _ptr(v_scale), int(prefix_len), int(chunk_len), int(capacity), int(n_q_heads),
+                                      int(n_kv_heads), int(head_dim), float(rope_base), _stream(stream))
+
+    @staticmethod
+    def chunk_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, scale, out,
+                      workspace, workspace_bytes, stream):
+        return _lib.kvra_chunk_attn_q8(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), int(prefix_len),
+                                       int(chunk_len), int(n_q_heads), int(n_kv_heads), int(head_dim), float(scale), _ptr(out),
+                                       _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+    @staticmethod
+    def pack_w4(w, codes, scales, n, k, stream):
+        return _lib.kvra_pack_w4(_ptr(w), _ptr(codes), _ptr(scales), int(n), int(k), _stream(stream))
+
+    @staticmethod
+    def unpack_w4(codes, scales, w, n, k, stream):
+        return _lib.kvra_unpack_w4(_ptr(codes), _ptr(scales), _ptr(w), int(n), int(k), _stream(stream))
+
+    @staticmethod
+    def linear_w4(x, w, w_scale, w2, w2_scale, residual, out, m, n, k, stream):
+        return _lib.kvra_linear_w4(_ptr(x), _ptr(w), _ptr(w_scale), _ptr(w2), _ptr(w2_scale), _ptr(residual), _ptr(out), int(m),
+                                   int(n), int(k), _stream(stream))
+
 
 def _load_calls():
     # The module is compiled against torch's C++ headers and this Python's: its file is named after both (one for another torch or
@@ -202,7 +229,8 @@ def _load_calls():
     loader = importlib.machinery.ExtensionFileLoader(name, path)
     calls = importlib.util.module_from_spec(importlib.util.spec_from_file_location(name, path, loader=loader))
     loader.exec_module(calls)
-    names = ("kvra_append_kv", "kvra_chunk_attn", "kvra_rms_norm", "kvra_linear", "kvra_qkv_proj", "kvra_layer_chunk")
+    names = ("kvra_append_kv", "kvra_chunk_attn", "kvra_rms_norm", "kvra_linear", "kvra_qkv_proj", "kvra_layer_chunk", "kvra_append_kv_q8",
+             "kvra_chunk_attn_q8", "kvra_pack_w4", "kvra_unpack_w4", "kvra_linear_w4")
     calls.bind(_ptr, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names))
     return calls
 
@@ -479,9 +507,8 @@ def kvra_layer_chunk(layer: KvraLayer, x, y, k_cache, v_cache, prefix_len, chunk
 
 def kvra_append_kv_q8(k_in, v_in, q_in, q_out, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len, capacity,
                       n_q_heads, n_kv_heads, head_dim, rope_base, stream=None, check=True) -> int:
-    rc = _lib.kvra_append_kv_q8(_ptr(k_in), _ptr(v_in), _ptr(q_in), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
-                                _ptr(v_scale), int(prefix_len), int(chunk_len), int(capacity), int(n_q_heads), int(n_kv_heads),
-                                int(head_dim), float(rope_base), _stream(stream))
+    rc = _call.append_kv_q8(k_in, v_in, q_in, q_out, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len, capacity,
+                            n_q_heads, n_kv_heads, head_dim, rope_base, stream)
     if check and rc != KVRA_OK:
         raise KvraError(rc, "kvra_append_kv_q8")
     return rc
@@ -489,9 +516,8 @@ def kvra_append_kv_q8(k_in, v_in, q_in, q_out, k_cache, v_cache, k_scale, v_scal
 
 def kvra_chunk_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim,
                        scale, out, workspace, workspace_bytes, stream=None, check=True) -> int:
-    rc = _lib.kvra_chunk_attn_q8(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), int(prefix_len),
-                                 int(chunk_len), int(n_q_heads), int(n_kv_heads), int(head_dim), float(scale), _ptr(out),
-                                 _ptr(workspace), int(workspace_bytes), _stream(stream))
+    rc = _call.chunk_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim,
+                             scale, out, workspace, workspace_bytes, stream)
     if check and rc != KVRA_OK:
         raise KvraError(rc, "kvra_chunk_attn_q8")
     return rc
@@ -502,19 +528,18 @@ def kvra_chunk_attn_q8_workspace_bytes() -> int:
 
 
 def kvra_pack_w4(w, codes, scales, n, k, stream=None):
-    rc = _lib.kvra_pack_w4(_ptr(w), _ptr(codes), _ptr(scales), int(n), int(k), _stream(stream))
+    rc = _call.pack_w4(w, codes, scales, n, k, stream)
     if rc != KVRA_OK:
         raise KvraError(rc, "kvra_pack_w4")
 
 
 def kvra_unpack_w4(codes, scales, w, n, k, stream=None):
-    rc = _lib.kvra_unpack_w4(_ptr(codes), _ptr(scales), _ptr(w), int(n), int(k), _stream(stream))
+    rc = _call.unpack_w4(codes, scales, w, n, k, stream)
     if rc != KVRA_OK:
         raise KvraError(rc, "kvra_unpack_w4")
 
 
 def kvra_linear_w4(x, w, w_scale, w2, w2_scale, residual, out, m, n, k, stream=None):
-    rc = _lib.kvra_linear_w4(_ptr(x), _ptr(w), _ptr(w_scale), _ptr(w2), _ptr(w2_scale), _ptr(residual), _ptr(out), int(m), int(n),
-                             int(k), _stream(stream))
+    rc = _call.linear_w4(x, w, w_scale, w2, w2_scale, residual, out, m, n, k, stream)
     if rc != KVRA_OK:
         raise KvraError(rc, "kvra_linear_w4")

@@ -150,3 +150,13 @@ def test_tensors_that_may_not_be_passed():
         _attn(workspace=t.t())
     with pytest.raises(ValueError):
         kvra.kvra_linear_w4(t, A[0], A[1], None, None, None, A[2], 1, 32, 64)
+
+
+def test_ctypes_does_the_same(monkeypatch):
+    monkeypatch.setattr(kvra, "_call", kvra._CtypesCalls)
+    for want, args in ((INVALID, dict(k_in=None)), (UNSUPPORTED, dict(d=96)), (RANGE, dict(p=63, c=2)), (INVALID, dict(base=math.nan))):
+        assert _append(**args) == want
+    for want, args in ((INVALID, dict(out=None)), (INVALID, dict(bytes_=1)), (INVALID, dict(scale=0.0)), (UNSUPPORTED, dict(d=32))):
+        assert _attn(**args) == want
+    test_weight_refusals()
+    test_tensors_that_may_not_be_passed()
