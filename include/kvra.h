@@ -401,7 +401,7 @@ int kvra_layer_chunk(const kvra_layer* layer, const void* x, void* y, void* k_ca
  * A block's exponent e is the smallest with which its largest finite magnitude does not overflow (<= 448 * 2^e,
  * <= 6 * 2^e), kept within -100 .. 120; values are rounded to nearest, ties to even.  A value of either format
  * times its scale is an exact bf16 number (e4m3: up to 248 * 2^120): the calls compute with those.
- * Tensors other than scales are 16-byte aligned (KVRA_EINVAL otherwise).
+ * Tensors are 16-byte aligned, scales of weights 2-byte (KVRA_EINVAL otherwise).
  */
 
 /*

@@ -360,7 +360,8 @@ extern "C" int kvra_linear_w4(const void* x, const void* w, const void* w_scale,
                               const void* residual, void* out, int64_t m, int64_t n, int64_t k, void* stream) {
   if (x == nullptr || w == nullptr || w_scale == nullptr || out == nullptr) return KVRA_EINVAL;
   if ((w2 == nullptr) != (w2_scale == nullptr) || (w2 != nullptr && residual != nullptr)) return KVRA_EINVAL;
-  if (!aligned(x) || !aligned(w) || !aligned(w2) || !aligned(residual) || !aligned(out)) return KVRA_EINVAL;
+  if (!aligned(x) || !aligned(w) || !aligned(w2) || !aligned(residual) || !aligned(out) || !aligned(w_scale, 2) || !aligned(w2_scale, 2))
+    return KVRA_EINVAL;
   int rc = check_linear(m, n, k);
   if (rc != KVRA_OK) return rc;
   return kvra::launch_linear_w4(x, w, w_scale, w2, w2_scale, residual, out, m, n, k, static_cast<hipStream_t>(stream));

@@ -6,6 +6,7 @@
 #include "kvra_lowbit_device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace kvra {
 
@@ -99,14 +100,20 @@ struct LinearW4Args {
   int k;
 };
 
-// Weights straight from memory into the A operand of v_mfma_f32_16x16x32_bf16: a lane loads 32 codes (16 bytes: one group of one
-// row) and feeds them to four products, whose contraction slots are therefore components 32 g + 8 i .. of 128.  The waves of a
-// workgroup share out k and meet in LDS.
-template <bool DUAL, int RB, int TB, int WAVES>
+// HBM-bound, and before that bound by the address unit: in the order of the A operand of v_mfma_f32_16x16x32_bf16, 16 neighbouring
+// lanes ask for 16 different rows, 64 lookups an instruction, and the weights came at 2.4 TB/s.  So four neighbouring lanes load
+// 64 bytes of a row, 128 of k, and a buffer of the wave in LDS turns them into operand order (LDS operations of a wave are carried out in
+// order: no barrier); the tokens go the same way, 256 bytes of a row to 16 lanes.  A lane's 16 bytes of codes are one group of one
+// row and feed four products, whose contraction slots are components 32 g + 8 i .. of the 128.  The waves of a workgroup share out k
+// and meet in LDS.  XL: loads of four tokens each.
+template <bool DUAL, int RB, int TB, int XL, int WAVES, int DEPTH>
 __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args a) {
   static_assert(!DUAL || RB % 2 == 0, "gate and up rows side by side");
+  static_assert(XL <= 4 * TB && 4 % DEPTH == 0, "");
   constexpr int OB = DUAL ? RB / 2 : RB;         // 16-row blocks of output columns
-  extern __shared__ f32x4 sums[];                // [wave][row block][token block][lane]
+  constexpr int BUF = (RB + 4 * TB) * 64;        // 16-byte pieces of a wave's buffer: codes, tokens
+  extern __shared__ u32x4 smem[];                // the waves' buffers; then [wave][row block][token block][lane]
+  f32x4* const sums = reinterpret_cast<f32x4*>(smem);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
@@ -115,59 +122,101 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
   const int chunks = (a.k + 127) / 128;
   const int c0 = chunks * wave / WAVES, c1 = chunks * (wave + 1) / WAVES;
 
+  // loading: lane / 4 is the row of a block and lane % 4 the group of a chunk; for tokens lane / 16 and lane % 16
   const unsigned char* w_row[RB];
   const unsigned char* s_row[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const long long row = n0 + 16 * (DUAL ? rb / 2 : rb) + r16;
+    const long long row = n0 + 16 * (DUAL ? rb / 2 : rb) + (lane >> 2);
     const bool up = DUAL && rb % 2 == 1;
-    w_row[rb] = (up ? a.w2 : a.w) + row * (a.k / 2) + 16 * g4;
-    s_row[rb] = (up ? a.ws2 : a.ws) + row * (a.k / 32) + g4;
+    w_row[rb] = (up ? a.w2 : a.w) + row * (a.k / 2) + 16 * (lane & 3);
+    s_row[rb] = (up ? a.ws2 : a.ws) + row * (a.k / 32);
   }
-  const __bf16* x_row[TB];
+  const __bf16* x_row[XL];
 #pragma unroll
-  for (int tb = 0; tb < TB; ++tb) x_row[tb] = a.x + static_cast<long long>(min(tok0 + 16 * tb + r16, a.m - 1)) * a.k + 32 * g4;
+  for (int i = 0; i < XL; ++i) x_row[i] = a.x + static_cast<long long>(min(tok0 + 4 * i + (lane >> 4), a.m - 1)) * a.k + 8 * (lane & 15);
+  struct Chunk {
+    u32x4 w[RB], x[XL];
+  };
+  // (what lies behind the end of a row is loaded as zeros: a half chunk, or one past the wave's share)
+  auto load = [&](Chunk& b, int c) __attribute__((always_inline)) {
+    const bool w_in = c < c1 && 128 * c + 32 * (lane & 3) < a.k, x_in = c < c1 && 128 * c + 8 * (lane & 15) < a.k;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      b.w[rb] = *reinterpret_cast<const u32x4*>(w_row[rb] + (w_in ? 64 * c : -16 * (lane & 3)));
+      if (!w_in) b.w[rb] = u32x4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+      b.x[i] = *reinterpret_cast<const u32x4*>(x_row[i] + (x_in ? 128 * c : -8 * (lane & 15)));
+      if (!x_in) b.x[i] = u32x4{0u, 0u, 0u, 0u};
+    }
+  };
+  // the four scales of chunk c + lane % 4 of a row
+  auto load_scales = [&](int rb, int c) __attribute__((always_inline)) -> unsigned {
+    const int at = 4 * (c + (lane & 3)), last = a.k / 32 - 2;    // (rows are an even number of bytes)
+    return *reinterpret_cast<const unsigned short*>(s_row[rb] + min(at, last)) |
+           static_cast<unsigned>(*reinterpret_cast<const unsigned short*>(s_row[rb] + min(at + 2, last))) << 16;
+  };
+
+  // the wave's buffer.  Slot of a row's piece: codes piece ^ f, f = 0, 3, 2, 1 for rows 0, 4, 8, 12 on; tokens piece ^ (row - 4) % 16: so
+  // that the eight lanes that read in one cycle ({0..3, 12..15} of a 16-lane row with {4..11} of the next) meet no bank twice
+  u32x4* const buf = smem + wave * BUF;
+  const int w_put = (lane >> 2) * 4 + ((lane & 3) ^ (-(lane >> 4) & 3));
+  const int x_put = (lane >> 4) * 16, x_get = RB * 64 + r16 * 16;
+  const int w_get = r16 * 4 + (g4 ^ (-(r16 >> 2) & 3));
 
   f32x4 acc[RB][TB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  Chunk ring[DEPTH];
+  unsigned scales[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) scales[rb] = load_scales(rb, c0);
+#pragma unroll
+  for (int u = 0; u < DEPTH; ++u) load(ring[u], c0 + u);
 
-  for (int c = c0; c < c1; ++c) {
-    u32x4 w[RB];
-    unsigned s[RB];
-    bf16x8 xf[TB][4];
-    if (128 * c + 32 * g4 < a.k) {
+  for (int c = c0; c < c1; c += 4) {
+    unsigned next[RB];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (c + u >= c1) break;
+      Chunk& b = ring[u % DEPTH];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) buf[rb * 64 + w_put] = b.w[rb];
+#pragma unroll
+      for (int i = 0; i < XL; ++i) buf[RB * 64 + i * 64 + x_put + ((lane & 15) ^ ((4 * i + (lane >> 4) - 4) & 15))] = b.x[i];
+      load(b, c + u + DEPTH);
+      if (u == 0)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) next[rb] = load_scales(rb, c + 4);
+      u32x4 w[RB];
+      float factor[RB];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        w[rb] = *reinterpret_cast<const u32x4*>(w_row[rb] + 64 * static_cast<long long>(c));
-        s[rb] = s_row[rb][4 * c];
+        w[rb] = buf[rb * 64 + w_get];
+        const unsigned four = static_cast<unsigned>(__builtin_amdgcn_ds_bpermute(4 * (4 * r16 + u), static_cast<int>(scales[rb])));
+        factor[rb] = scale_factor(four >> (8 * g4) & 255u);
       }
 #pragma unroll
-      for (int tb = 0; tb < TB; ++tb)
+      for (int i = 0; i < 4; ++i) {
+        bf16x8 x[TB];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) xf[tb][i] = *reinterpret_cast<const bf16x8*>(x_row[tb] + 128 * static_cast<long long>(c) + 8 * i);
-    } else {                                     // behind the end of the rows
+        for (int tb = 0; tb < TB; ++tb) x[tb] = __builtin_bit_cast(bf16x8, buf[x_get + tb * 256 + ((4 * g4 + i) ^ ((r16 - 4) & 15))]);
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        w[rb] = u32x4{0u, 0u, 0u, 0u};
-        s[rb] = 127;
+        for (int rb = 0; rb < RB; ++rb) {
+          const bf16x8 wx = dequant8(w[rb][i], factor[rb]);
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx, x[tb], acc[rb][tb], 0, 0, 0);
+        }
       }
-#pragma unroll
-      for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) xf[tb][i] = bf16x8{};
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const bf16x8 wf = dequant8(w[rb][i], scale_factor(s[rb]));
-#pragma unroll
-        for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[tb][i], acc[rb][tb], 0, 0, 0);
-      }
+    for (int rb = 0; rb < RB; ++rb) scales[rb] = next[rb];
   }
+  __syncthreads();
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -204,16 +253,21 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
 }
 
 // ---- many tokens -------------------------------------------------------------------------------------------------------
-// MFMA-bound.  A wave owns 64 weight rows x 64 tokens: per 128 of k it converts 64 x 128 codes (64 conversions, on the vector
-// pipe) for 64 matrix products.  Codes go from memory to registers in operand order as above, one stage ahead; tokens go to LDS
-// (16 KB a stage, loaded straight to it, two stages), where the WN waves of a workgroup that have the same k share them.  WK waves share
-// the k of a tile and meet in LDS at the end, so that a launch of few tiles still fills the chip.
+// MFMA-bound.  A wave owns 64 weight rows x 64 tokens: per stage of 128 of k it converts 64 x 128 codes (64 conversions, on the
+// vector pipe, beside the products) for 64 matrix products.  Codes and tokens go straight to LDS, the codes to the wave's own (4 KB a
+// stage, two stages), the tokens to a ring of three stages of 16 KB that the four waves with the same k share.  A
+// stage is 16 steps of four products; between them lie, each a step or more ahead of its use: one operand read, the conversion of one
+// weight operand, the loads of the next stages, and the one barrier, past which a stage's reads begin three quarters of a stage later.
+// WK groups of four waves share the k of a tile and meet in LDS at the end, so that one workgroup per CU has two waves per SIMD.
 constexpr int kTileStage = 64 * 256;      // bytes: 64 tokens x 128 of k
+constexpr int kTileRing = 3;
+constexpr int kTileCodes = 64 * 64;       // of a wave: 64 rows x 128 of k
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4_w4;
 
-template <bool DUAL, int WN, int WK>
-__global__ __launch_bounds__(64 * WN * WK, 2) void linear_w4_tile_kernel(LinearW4Args a) {
-  constexpr int TK = 128;                 // k of a stage
-  extern __shared__ u32x4 smem[];         // [wk][2 stages]; at the end the sums of the waves with wk > 0
+template <bool DUAL, int WK>
+__global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Args a) {
+  constexpr int TK = 128, WN = 4;         // k of a stage; waves along the weight rows
+  extern __shared__ u32x4 smem[];         // [wk][ring]; at the end the sums of the waves with wk > 0
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = wave % WN, wk = wave / WN;
@@ -225,53 +279,65 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void linear_w4_tile_kernel(LinearW
   if ((blockIdx.x >> 3) >= static_cast<unsigned>(per) || tile >= tiles) return;   // the whole workgroup
   const int tok0 = tile % token_tiles * 64, n0 = tile / token_tiles * (COLS * WN) + wn * COLS;
 
-  const int stages_all = (a.k + TK - 1) / TK;
-  const int s0 = stages_all * wk / WK, s1 = stages_all * (wk + 1) / WK, stages = (stages_all + WK - 1) / WK;   // (of the longest share)
+  // this group's stages [s0, s1), of which the last of all may be half a one (k = 64 mod 128): `whole` stages and then that
+  const int stages = (a.k + TK - 1) / TK;
+  const int s0 = stages * wk / WK, s1 = stages * (wk + 1) / WK, whole = min(s1, a.k / TK) - s0, longest = (stages + WK - 1) / WK;
 
   // weights: row blocks 0..3; SwiGLU: gate rows in 0 and 1, the same rows of up in 2 and 3.  Rows past the end repeat the last.
-  const unsigned char* w_row[4];
-  const unsigned char* s_row[4];
+  // Loads as in the kernel for few tokens, four neighbouring lanes to 64 bytes of a row, but straight to the wave's LDS (two stages);
+  // scales by lane = row, 16 bytes for four stages, and from lane to lane.  (A scale load's wait drains the loads sent before it:
+  // once in four stages.)
+  auto row_of = [&](int rb, int r) __attribute__((always_inline)) -> long long { return min(n0 + 16 * (DUAL ? rb % 2 : rb) + r, a.n - 1); };
+  auto resource = [](const void* at, unsigned long long bytes) __attribute__((always_inline)) -> u32x4 {
+    const unsigned long long p = reinterpret_cast<unsigned long long>(at);
+    return u32x4{static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(p))),
+                 static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32))) & 0xFFFFu,
+                 static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(bytes))), 0x00020000u};
+  };
+  const u32x4 w_res = resource(a.w, static_cast<unsigned long long>(a.n) * (a.k / 2)), w2_res = DUAL ? resource(a.w2, static_cast<unsigned long long>(a.n) * (a.k / 2)) : w_res;
+  unsigned w_off[4];
 #pragma unroll
-  for (int rb = 0; rb < 4; ++rb) {
-    const bool up = DUAL && rb >= 2;
-    const long long row = min(n0 + 16 * (DUAL ? rb % 2 : rb) + r16, a.n - 1);
-    w_row[rb] = (up ? a.w2 : a.w) + row * (a.k / 2) + 16 * g4;
-    s_row[rb] = (up ? a.ws2 : a.ws) + row * (a.k / 32) + g4;
-  }
-  u32x4 w[4];
-  unsigned ws[4];
-  auto load_w = [&](int st) __attribute__((always_inline)) {
-    const bool in = TK * st + 32 * g4 < a.k;      // (the last stage of k = 64 mod 128 has half of it)
-#pragma unroll
-    for (int rb = 0; rb < 4; ++rb) {
-      w[rb] = u32x4{0u, 0u, 0u, 0u};
-      ws[rb] = 127;
-      if (in) {
-        w[rb] = *reinterpret_cast<const u32x4*>(w_row[rb] + 64 * static_cast<long long>(st));
-        ws[rb] = s_row[rb][4 * st];
-      }
-    }
+  for (int rb = 0; rb < 4; ++rb) w_off[rb] = static_cast<unsigned>(row_of(rb, lane >> 2) * (a.k / 2)) + 16 * ((lane & 3) ^ (-(lane >> 4) & 3));
+  const unsigned lds_w = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)smem)) + WK * kTileRing * kTileStage + wave * 2 * kTileCodes;
+  auto load_w = [&](int rb, int st, unsigned half) __attribute__((always_inline)) {
+    lds_dma16(DUAL && rb >= 2 ? w2_res : w_res, w_off[rb] + 64 * static_cast<unsigned>(st), lds_w + half + rb * 1024);
+  };
+  const unsigned w_addr = lds_w + r16 * 64 + (g4 ^ (-(r16 >> 2) & 3)) * 16;
+  auto read_w = [&](int rb, unsigned half) __attribute__((always_inline)) -> u32x4 {
+    return *(lds_u32x4_w4*)static_cast<uintptr_t>(w_addr + half + rb * 1024);
+  };
+  const unsigned char* const s_row = (DUAL && lane >= 32 ? a.ws2 : a.ws) + row_of(lane >> 4, r16) * (a.k / 32);
+  u32x4 scales, scales_next;
+  auto load_scales = [&](int st) __attribute__((always_inline)) -> u32x4 {
+    u32x4 v;
+    __builtin_memcpy(&v, s_row + min(16 * (st >> 2), a.k / 32 - 16), 16);
+    return v;
+  };
+  // the factor of row block rb in stage st: byte g4 of the four that lane 16 rb + r16 holds for the stage
+  auto stage_scales = [&](const u32x4& v, int st) __attribute__((always_inline)) -> unsigned {
+    const int at = 4 * st - min(16 * (st >> 2), a.k / 32 - 16);
+    const unsigned lo = at & 8 ? (at & 4 ? v[3] : v[2]) : (at & 4 ? v[1] : v[0]), hi = at & 8 ? v[3] : (at & 4 ? v[2] : v[1]);
+    return at & 2 ? lo >> 16 | hi << 16 : lo;    // (k = 64 mod 128: the last stages' begin between two words)
+  };
+  auto factor_of = [&](int rb, unsigned four) __attribute__((always_inline)) -> float {
+    return scale_factor(static_cast<unsigned>(__builtin_amdgcn_ds_bpermute(4 * (16 * rb + r16), static_cast<int>(four))) >> (8 * g4) & 255u);
   };
 
-  // tokens: a row of a stage is 16 pieces of 16 bytes; slot = piece ^ (row % 16), so that 16 rows of one piece meet no bank twice
-  const unsigned long long x_at = reinterpret_cast<unsigned long long>(a.x) + static_cast<unsigned long long>(tok0) * a.k * 2;
-  const unsigned long long x_left = static_cast<unsigned long long>(a.m - tok0) * a.k * 2;   // (below 4 GiB); beyond: zeros
-  const u32x4 x_res = {static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(x_at))),
-                       static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(x_at >> 32))) & 0xFFFFu,
-                       static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(x_left))), 0x00020000u};
-  const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)smem)) + wk * 2 * kTileStage;
-  constexpr int LOADS = 16 / WN;          // of this wave, 4 rows each
-  const unsigned x_row = static_cast<unsigned>(4 * wn + (lane >> 4)) * a.k * 2, x_piece = static_cast<unsigned>((lane & 15) ^ (lane >> 4)) * 16;
-  auto load_x = [&](int st) __attribute__((always_inline)) {
-    unsigned row = x_row + static_cast<unsigned>(st) * 256, piece = x_piece, step = 4 * WN * static_cast<unsigned>(a.k) * 2;
-    asm volatile("" : "+v"(row), "+v"(piece), "+s"(step));   // (opaque, so that nothing is formed ahead and kept)
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-      lds_dma16(x_res, (piece ^ 64u * ((i * WN + wn) & 3)) + row + i * step, lds0 + (st & 1) * kTileStage + (i * WN + wn) * 1024);
+  // tokens: a row of a stage is 16 pieces of 16 bytes; slot = piece ^ (row - 4) % 16, for the banks' sake
+  const u32x4 x_res = resource(a.x + static_cast<long long>(tok0) * a.k, static_cast<unsigned long long>(a.m - tok0) * a.k * 2);   // beyond: zeros
+  const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)smem)) + wk * kTileRing * kTileStage;
+  // load i of this wave: rows 16 i + 4 wn ..
+  const unsigned x_row = static_cast<unsigned>(4 * wn + (lane >> 4)) * a.k * 2 +
+                         (static_cast<unsigned>((lane & 15) ^ (lane >> 4)) * 16 ^ 64u * ((wn + 3) & 3)), x_step = 16 * static_cast<unsigned>(a.k) * 2;
+  auto load_x = [&](int i, int st, unsigned slot) __attribute__((always_inline)) {
+    lds_dma16(x_res, x_row + i * x_step + static_cast<unsigned>(st) * 256, lds0 + slot + (i * WN + wn) * 1024);
   };
   unsigned x_addr[4];                     // of product i: token r16's piece 4 g4 + i
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x_addr[i] = lds0 + r16 * 256 + ((4 * g4 + i) ^ r16) * 16;
+  for (int i = 0; i < 4; ++i) x_addr[i] = lds0 + r16 * 256 + ((4 * g4 + i) ^ ((r16 - 4) & 15)) * 16;
+  auto read_x = [&](int i, int tb, unsigned slot) __attribute__((always_inline)) -> bf16x8 {
+    return *(lds_bf16x8*)static_cast<uintptr_t>(x_addr[i] + slot + tb * 16 * 256);
+  };
 
   f32x4 acc[4][4];
 #pragma unroll
@@ -279,46 +345,100 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void linear_w4_tile_kernel(LinearW
 #pragma unroll
     for (int tb = 0; tb < 4; ++tb) acc[rb][tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
+  u32x4 w[2][4];
+  float f[2][4];
+  bf16x8 x[2][4], wx[2];
+  unsigned slot = 0, slot1 = kTileStage, slot2 = 2 * kTileStage;   // of this stage's tokens, the next one's, those after
   if (s0 < s1) {
-    load_x(s0);
-    load_w(s0);
+    scales = load_scales(s0);
+    scales_next = load_scales(min(s0 + 4, s1 - 1));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      load_x(i, s0, slot);
+      load_x(i, min(s0 + 1, s1 - 1), slot1);
+      load_w(i, s0, 0);
+      load_w(i, min(s0 + 1, s1 - 1), kTileCodes);
+    }
   }
-  for (int j = 0; j < stages; ++j) {
-    const int st = s0 + j;
-    u32x4 wc[4];
-    float wf[4];
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
 #pragma unroll
-    for (int rb = 0; rb < 4; ++rb) {
-      wc[rb] = w[rb];
-      wf[rb] = scale_factor(ws[rb]);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();                      // the stage is there for all its waves, and all have read the one before
-    if (st + 1 < s1) {
-      load_x(st + 1);
-      load_w(st + 1);
-    }
-    if (st < s1) {
-      const unsigned slot = (st & 1) * kTileStage;
-      const bool in = TK * st + 32 * g4 < a.k;
+  for (int i = 0; i < 4; ++i) {
+    x[0][i] = read_x(0, i, slot);
+    w[0][i] = read_w(i, 0);
+    f[0][i] = factor_of(i, stage_scales(scales, s0));
+  }
+  wx[0] = dequant8(w[0][0][0], f[0][0]);
+
+  // One whole stage, the H-th of a pair: its weights are in w[H]; the next one's are read to the other.
+  auto stage = [&](int st, auto half_tag) __attribute__((always_inline)) {
+    constexpr int H = decltype(half_tag)::value;
+    constexpr unsigned HERE = H * kTileCodes, OTHER = kTileCodes - HERE;
+    const int st1 = min(st + 1, s1 - 1), st2 = min(st + 2, s1 - 1);   // (past the end: loaded again, to where nobody looks)
+    unsigned four = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bf16x8 x[4];
-#pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-          x[tb] = *(lds_bf16x8*)static_cast<uintptr_t>(x_addr[i] + slot + tb * 16 * 256);
-          if (!in) x[tb] = bf16x8{};      // (what lies behind the end of a row belongs to the next token)
-        }
-#pragma unroll
-        for (int rb = 0; rb < 4; ++rb) {
-          const bf16x8 wx = dequant8(wc[rb][i], wf[rb]);
-#pragma unroll
-          for (int tb = 0; tb < 4; ++tb) acc[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx, x[tb], acc[rb][tb], 0, 0, 0);
-        }
+    for (int q = 0; q < 16; ++q) {
+      const int i = q / 4, rb = q % 4;
+      __builtin_amdgcn_sched_barrier(0);
+      x[(i + 1) % 2][rb] = i < 3 ? read_x(i + 1, rb, slot) : read_x(0, rb, slot1);
+      if (q == 10 && (st1 & 3) == 0 && st1 != st) {
+        scales = scales_next;
+        scales_next = load_scales(min(st1 + 4, s1 - 1));
       }
+      if (q == 10) four = stage_scales(scales, st1);
+      if (q >= 11 && q < 15) {
+        if (q == 11) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");   // the next stage's codes: all but this stage's loads
+        w[1 - H][q - 11] = read_w(q - 11, OTHER);
+        f[1 - H][q - 11] = factor_of(q - 11, four);
+      }
+      const int q1 = (q + 1) % 16, from = q < 15 ? H : 1 - H;
+      wx[q1 % 2] = dequant8(w[from][q1 % 4][q1 / 4], f[from][q1 % 4]);
+      if (q == 1) {   // every wave of the group is done with the stage before, and the next one's tokens are there
+        asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      if (q >= 2 && q < 6) load_x(q - 2, st2, slot2);
+      if (q >= 6 && q < 10) load_w(q - 6, st2, HERE);
+#pragma unroll
+      for (int tb = 0; tb < 4; ++tb) acc[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wx[q % 2], x[i % 2][tb], acc[rb][tb], 0, 0, 0);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    const unsigned done = slot;
+    slot = slot1;
+    slot1 = slot2;
+    slot2 = done;
+  };
+  int j = 0;
+  for (; j + 2 <= whole; j += 2) {
+    stage(s0 + j, std::integral_constant<int, 0>{});
+    stage(s0 + j + 1, std::integral_constant<int, 1>{});
+  }
+  if (j < whole) {
+    stage(s0 + j, std::integral_constant<int, 0>{});
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[0][i] = w[1][i];
+      f[0][i] = f[1][i];
+    }
+    ++j;
+  }
+  for (int b = j; b < longest; ++b) __builtin_amdgcn_s_barrier();     // (as many barriers for every group)
+  if (whole < s1 - s0) {                  // the half stage
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int tb = 0; tb < 4; ++tb) {
+        // what lies behind the end of a row belongs to the next token
+        const bf16x8 xt = g4 < 2 ? read_x(i, tb, slot) : bf16x8{};
+#pragma unroll
+        for (int rb = 0; rb < 4; ++rb)
+          acc[rb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dequant8(g4 < 2 ? w[0][rb][i] : 0u, g4 < 2 ? f[0][rb] : 1.0f), xt,
+                                                                acc[rb][tb], 0, 0, 0);
+      }
   }
 
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if constexpr (WK > 1) {
     __syncthreads();
     f32x4* const sums = reinterpret_cast<f32x4*>(smem);     // [wk - 1][wn][block][lane]
@@ -363,29 +483,37 @@ __global__ __launch_bounds__(64 * WN * WK, 2) void linear_w4_tile_kernel(LinearW
 
 namespace {
 
-template <bool DUAL, int RB, int TB, int WAVES>
+template <bool DUAL, int RB, int TB, int XL, int WAVES, int DEPTH>
 int launch_rows(LinearW4Args& a, hipStream_t stream) {
   const int64_t tiles = (a.m + 16 * TB - 1) / (16 * TB);
   if (tiles > 65535) return KVRA_EUNSUPPORTED;
-  return launch_kernel(linear_w4_rows_kernel<DUAL, RB, TB, WAVES>, dim3(static_cast<unsigned>(a.n / (DUAL ? 8 * RB : 16 * RB)), static_cast<unsigned>(tiles)),
-                       dim3(64 * WAVES), a, stream, WAVES * RB * TB * 64u * 16u);
+  return launch_kernel(linear_w4_rows_kernel<DUAL, RB, TB, XL, WAVES, DEPTH>,
+                       dim3(static_cast<unsigned>(a.n / (DUAL ? 8 * RB : 16 * RB)), static_cast<unsigned>(tiles)), dim3(64 * WAVES), a, stream,
+                       WAVES * (RB + 4 * TB) * 1024u);
 }
 
-template <bool DUAL, int WN, int WK>
+template <bool DUAL>
+int launch_few(LinearW4Args& a, hipStream_t stream) {
+  constexpr int RB = DUAL ? 2 : 1;
+  if (a.m <= 4) return launch_rows<DUAL, RB, 1, 1, 8, 4>(a, stream);
+  if (a.m <= 16) return launch_rows<DUAL, RB, 1, 4, 8, 4>(a, stream);
+  if (a.m <= 32) return launch_rows<DUAL, 2, 2, 8, 8, 2>(a, stream);
+  return launch_rows<DUAL, 2, 4, 16, 8, 1>(a, stream);
+}
+
+template <bool DUAL, int WK>
 int launch_tile(LinearW4Args& a, hipStream_t stream) {
-  const int64_t token_tiles = (a.m + 63) / 64, cols = (DUAL ? 32 : 64) * WN, tiles = token_tiles * ((a.n + cols - 1) / cols);
+  const int64_t token_tiles = (a.m + 63) / 64, cols = DUAL ? 128 : 256, tiles = token_tiles * ((a.n + cols - 1) / cols);
   const int64_t grid = (tiles + 7) / 8 * 8;
   if (grid > INT32_MAX) return KVRA_EUNSUPPORTED;
-  const unsigned smem = std::max(WK * 2 * kTileStage, (WK - 1) * WN * 16 * 1024);
-  return launch_kernel(linear_w4_tile_kernel<DUAL, WN, WK>, dim3(static_cast<unsigned>(grid)), dim3(64 * WN * WK), a, stream, smem);
+  return launch_kernel(linear_w4_tile_kernel<DUAL, WK>, dim3(static_cast<unsigned>(grid)), dim3(256 * WK), a, stream,
+                       WK * (kTileRing * kTileStage + 4 * 2 * kTileCodes));
 }
 
 template <bool DUAL>
 int launch_many(LinearW4Args& a, hipStream_t stream) {
-  const int64_t tiles = static_cast<int64_t>((a.m + 63) / 64) * ((a.n + (DUAL ? 31 : 63)) / (DUAL ? 32 : 64));   // of one wave
-  if (tiles >= 4 * 384) return launch_tile<DUAL, 4, 1>(a, stream);
-  if (tiles >= 2 * 256) return launch_tile<DUAL, 2, 2>(a, stream);
-  return launch_tile<DUAL, 1, 4>(a, stream);
+  const int64_t tiles = static_cast<int64_t>((a.m + 63) / 64) * ((a.n + (DUAL ? 127 : 255)) / (DUAL ? 128 : 256));
+  return tiles > 256 ? launch_tile<DUAL, 1>(a, stream) : launch_tile<DUAL, 2>(a, stream);
 }
 
 }  // namespace
@@ -403,9 +531,9 @@ int launch_linear_w4(const void* x, const void* w, const void* ws, const void* w
   a.m = static_cast<int>(m);
   a.n = static_cast<int>(n);
   a.k = static_cast<int>(k);
-  if (m > 64) return w2 != nullptr ? launch_many<true>(a, stream) : launch_many<false>(a, stream);
-  if (w2 != nullptr) return m <= 16 ? launch_rows<true, 2, 1, 8>(a, stream) : launch_rows<true, 2, 4, 8>(a, stream);
-  return m <= 16 ? launch_rows<false, 1, 1, 8>(a, stream) : launch_rows<false, 1, 4, 8>(a, stream);
+  const bool dual = w2 != nullptr;
+  if (m <= 64 || k < 512) return dual ? launch_few<true>(a, stream) : launch_few<false>(a, stream);
+  return dual ? launch_many<true>(a, stream) : launch_many<false>(a, stream);
 }
 
 }  // namespace kvra

@@ -138,7 +138,7 @@ def test_weight_refusals():
         assert _code(call, a[0], a[1], a[2], 1 << 20, 1 << 12) == UNSUPPORTED
     lin = lambda x=a[0], w=a[1], s=a[2], w2=None, s2=None, r=None, o=a[3], m=1, n=32, k=64: _code(kvra.kvra_linear_w4, x, w, s, w2, s2, r, o, m, n, k)
     assert lin(x=None) == lin(w=None) == lin(s=None) == lin(o=None) == lin(w2=a[4]) == lin(s2=a[4]) == INVALID
-    assert lin(w2=a[4], s2=a[5], r=a[6]) == lin(x=4104) == lin(w=4104) == lin(r=4104) == lin(o=4104) == lin(m=0) == INVALID
+    assert lin(w2=a[4], s2=a[5], r=a[6]) == lin(x=4104) == lin(w=4104) == lin(r=4104) == lin(o=4104) == lin(m=0) == lin(s=4097) == lin(w2=a[4], s2=4097) == INVALID
     assert lin(n=48) == lin(k=32) == lin(m=1 << 20, k=1 << 12) == lin(m=(1 << 24) + 1) == UNSUPPORTED
 
 
