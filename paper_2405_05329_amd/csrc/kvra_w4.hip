@@ -106,10 +106,10 @@ struct LinearW4Args {
 // order: no barrier); the tokens go the same way, 256 bytes of a row to 16 lanes.  A lane's 16 bytes of codes are one group of one
 // row and feed four products, whose contraction slots are components 32 g + 8 i .. of the 128.  The waves of a workgroup share out k
 // and meet in LDS.  XL: loads of four tokens each.
-template <bool DUAL, int RB, int TB, int XL, int WAVES, int DEPTH>
+template <bool DUAL, int RB, int TB, int XL, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args a) {
   static_assert(!DUAL || RB % 2 == 0, "gate and up rows side by side");
-  static_assert(XL <= 4 * TB && 4 % DEPTH == 0, "");
+  static_assert(XL <= 4 * TB, "");
   constexpr int OB = DUAL ? RB / 2 : RB;         // 16-row blocks of output columns
   constexpr int BUF = (RB + 4 * TB) * 64;        // 16-byte pieces of a wave's buffer: codes, tokens
   extern __shared__ u32x4 smem[];                // the waves' buffers; then [wave][row block][token block][lane]
@@ -122,41 +122,42 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
   const int chunks = (a.k + 127) / 128;
   const int c0 = chunks * wave / WAVES, c1 = chunks * (wave + 1) / WAVES;
 
-  // loading: lane / 4 is the row of a block and lane % 4 the group of a chunk; for tokens lane / 16 and lane % 16
-  const unsigned char* w_row[RB];
-  const unsigned char* s_row[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const long long row = n0 + 16 * (DUAL ? rb / 2 : rb) + (lane >> 2);
-    const bool up = DUAL && rb % 2 == 1;
-    w_row[rb] = (up ? a.w2 : a.w) + row * (a.k / 2) + 16 * (lane & 3);
-    s_row[rb] = (up ? a.ws2 : a.ws) + row * (a.k / 32);
-  }
-  const __bf16* x_row[XL];
-#pragma unroll
-  for (int i = 0; i < XL; ++i) x_row[i] = a.x + static_cast<long long>(min(tok0 + 4 * i + (lane >> 4), a.m - 1)) * a.k + 8 * (lane & 15);
+  // loading: lane / 4 is the row of a block and lane % 4 the group of a chunk; for tokens lane / 16 and lane % 16.  Through buffer
+  // resources: one lane-constant offset a block, the chunk's in a scalar register, zeros behind the last row.
+  constexpr int MATS = DUAL ? 2 : 1;
+  auto resource = [](const void* at, unsigned bytes) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(at), 0, static_cast<int>(bytes), 0x00020000);
+  };
+  const unsigned w_ld = static_cast<unsigned>(a.k) / 2, s_ld = static_cast<unsigned>(a.k) / 32, x_ld = static_cast<unsigned>(a.k) * 2;
+  const __amdgpu_buffer_rsrc_t w_res[2] = {resource(a.w + static_cast<long long>(n0) * w_ld, 16 * OB * w_ld), resource((DUAL ? a.w2 : a.w) + static_cast<long long>(n0) * w_ld, 16 * OB * w_ld)};
+  const __amdgpu_buffer_rsrc_t s_res[2] = {resource(a.ws + static_cast<long long>(n0) * s_ld, 16 * OB * s_ld), resource((DUAL ? a.ws2 : a.ws) + static_cast<long long>(n0) * s_ld, 16 * OB * s_ld)};
+  const __amdgpu_buffer_rsrc_t x_res = resource(a.x + static_cast<long long>(tok0) * a.k, static_cast<unsigned>(a.m - tok0) * x_ld);
+  const unsigned w_off = static_cast<unsigned>(lane >> 2) * w_ld + 16 * (lane & 3), s_off = static_cast<unsigned>(lane >> 2) * s_ld;
+  const unsigned x_off = static_cast<unsigned>(lane >> 4) * x_ld + 16 * (lane & 15);
+  const bool words = (s_ld & 3) == 0;            // a chunk's four scales are a word
   struct Chunk {
     u32x4 w[RB], x[XL];
   };
-  // (what lies behind the end of a row is loaded as zeros: a half chunk, or one past the wave's share)
+  // (Chunks behind the wave's share are loaded and left.)
   auto load = [&](Chunk& b, int c) __attribute__((always_inline)) {
-    const bool w_in = c < c1 && 128 * c + 32 * (lane & 3) < a.k, x_in = c < c1 && 128 * c + 8 * (lane & 15) < a.k;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      b.w[rb] = *reinterpret_cast<const u32x4*>(w_row[rb] + (w_in ? 64 * c : -16 * (lane & 3)));
-      if (!w_in) b.w[rb] = u32x4{0u, 0u, 0u, 0u};
-    }
+    for (int rb = 0; rb < RB; ++rb)
+      b.w[rb] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w_res[rb % MATS], static_cast<int>(w_off + rb / MATS * 16 * w_ld), 64 * c, 0));
 #pragma unroll
-    for (int i = 0; i < XL; ++i) {
-      b.x[i] = *reinterpret_cast<const u32x4*>(x_row[i] + (x_in ? 128 * c : -8 * (lane & 15)));
-      if (!x_in) b.x[i] = u32x4{0u, 0u, 0u, 0u};
-    }
+    for (int i = 0; i < XL; ++i)
+      b.x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(x_res, static_cast<int>(x_off + 4 * i * x_ld), 256 * c, 0));
   };
-  // the four scales of chunk c + lane % 4 of a row
-  auto load_scales = [&](int rb, int c) __attribute__((always_inline)) -> unsigned {
-    const int at = 4 * (c + (lane & 3)), last = a.k / 32 - 2;    // (rows are an even number of bytes)
-    return *reinterpret_cast<const unsigned short*>(s_row[rb] + min(at, last)) |
-           static_cast<unsigned>(*reinterpret_cast<const unsigned short*>(s_row[rb] + min(at + 2, last))) << 16;
+  // The four scales of chunk c + lane % 4 of a row.  (Behind the end of the row: the row's last, so that what the half chunk's
+  // zeros are multiplied with is NaN only where the row is.)
+  struct Four {
+    unsigned lo, hi;
+  };
+  auto load_scales = [&](int rb, int c) __attribute__((always_inline)) -> Four {
+    const int at = 4 * (c + (lane & 3)), row = static_cast<int>(s_off + rb / MATS * 16 * s_ld);
+    if (words) return {__builtin_amdgcn_raw_buffer_load_b32(s_res[rb % MATS], row + min(at, static_cast<int>(s_ld) - 4), 0, 0), 0u};
+    const int last = static_cast<int>(s_ld) - 2;   // (rows are an even number of bytes)
+    return {__builtin_amdgcn_raw_buffer_load_b16(s_res[rb % MATS], row + min(at, last), 0, 0),
+            __builtin_amdgcn_raw_buffer_load_b16(s_res[rb % MATS], row + min(at + 2, last), 0, 0)};
   };
 
   // the wave's buffer.  Slot of a row's piece: codes piece ^ f, f = 0, 3, 2, 1 for rows 0, 4, 8, 12 on; tokens piece ^ (row - 4) % 16: so
@@ -171,24 +172,26 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
     for (int tb = 0; tb < TB; ++tb) acc[rb][tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  Chunk ring[DEPTH];
-  unsigned scales[RB];
+  Chunk b;                                       // one chunk ahead: more waves on a CU beat more loads in a wave
+  Four scales[RB];
+  load(b, c0);
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) scales[rb] = load_scales(rb, c0);
-#pragma unroll
-  for (int u = 0; u < DEPTH; ++u) load(ring[u], c0 + u);
 
   for (int c = c0; c < c1; c += 4) {
-    unsigned next[RB];
+    Four next[RB];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (c + u >= c1) break;
-      Chunk& b = ring[u % DEPTH];
+      if (128 * (c + u) + 128 > a.k && (lane & 15) >= 8) {   // the half chunk: what follows is the next token's
+#pragma unroll
+        for (int i = 0; i < XL; ++i) b.x[i] = u32x4{0u, 0u, 0u, 0u};
+      }
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) buf[rb * 64 + w_put] = b.w[rb];
 #pragma unroll
       for (int i = 0; i < XL; ++i) buf[RB * 64 + i * 64 + x_put + ((lane & 15) ^ ((4 * i + (lane >> 4) - 4) & 15))] = b.x[i];
-      load(b, c + u + DEPTH);
+      load(b, c + u + 1);
       if (u == 0)
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) next[rb] = load_scales(rb, c + 4);
@@ -197,7 +200,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         w[rb] = buf[rb * 64 + w_get];
-        const unsigned four = static_cast<unsigned>(__builtin_amdgcn_ds_bpermute(4 * (4 * r16 + u), static_cast<int>(scales[rb])));
+        const unsigned four = static_cast<unsigned>(__builtin_amdgcn_ds_bpermute(4 * (4 * r16 + u), static_cast<int>(scales[rb].lo | scales[rb].hi << 16)));
         factor[rb] = scale_factor(four >> (8 * g4) & 255u);
       }
 #pragma unroll
@@ -483,11 +486,11 @@ __global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Arg
 
 namespace {
 
-template <bool DUAL, int RB, int TB, int XL, int WAVES, int DEPTH>
+template <bool DUAL, int RB, int TB, int XL, int WAVES>
 int launch_rows(LinearW4Args& a, hipStream_t stream) {
   const int64_t tiles = (a.m + 16 * TB - 1) / (16 * TB);
   if (tiles > 65535) return KVRA_EUNSUPPORTED;
-  return launch_kernel(linear_w4_rows_kernel<DUAL, RB, TB, XL, WAVES, DEPTH>,
+  return launch_kernel(linear_w4_rows_kernel<DUAL, RB, TB, XL, WAVES>,
                        dim3(static_cast<unsigned>(a.n / (DUAL ? 8 * RB : 16 * RB)), static_cast<unsigned>(tiles)), dim3(64 * WAVES), a, stream,
                        WAVES * (RB + 4 * TB) * 1024u);
 }
@@ -495,10 +498,10 @@ int launch_rows(LinearW4Args& a, hipStream_t stream) {
 template <bool DUAL>
 int launch_few(LinearW4Args& a, hipStream_t stream) {
   constexpr int RB = DUAL ? 2 : 1;
-  if (a.m <= 4) return launch_rows<DUAL, RB, 1, 1, 8, 4>(a, stream);
-  if (a.m <= 16) return launch_rows<DUAL, RB, 1, 4, 8, 4>(a, stream);
-  if (a.m <= 32) return launch_rows<DUAL, 2, 2, 8, 8, 2>(a, stream);
-  return launch_rows<DUAL, 2, 4, 16, 8, 1>(a, stream);
+  if (a.m <= 4) return launch_rows<DUAL, RB, 1, 1, 8>(a, stream);
+  if (a.m <= 16) return launch_rows<DUAL, RB, 1, 4, 8>(a, stream);
+  if (a.m <= 32) return launch_rows<DUAL, 2, 2, 8, 8>(a, stream);
+  return launch_rows<DUAL, 2, 4, 16, 8>(a, stream);
 }
 
 template <bool DUAL, int WK>
