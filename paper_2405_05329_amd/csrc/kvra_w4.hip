@@ -276,11 +276,14 @@ __global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Arg
   const int wn = wave % WN, wk = wave / WN;
   const int r16 = lane & 15, g4 = lane >> 4;
   constexpr int COLS = DUAL ? 32 : 64;    // output columns of a wave
-  // ids go round-robin over the 8 XCDs: each takes a run of the order "token tile fastest"
+  // ids go round-robin over the 8 XCDs: each takes a run of the order "bands of token tiles, in a band token tile fastest", so
+  // that what an XCD runs together shares its tokens and weights in the L2
   const int token_tiles = (a.m + 63) / 64, col_tiles = (a.n + COLS * WN - 1) / (COLS * WN), tiles = token_tiles * col_tiles;
   const int per = (tiles + 7) / 8, tile = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((blockIdx.x >> 3) >= static_cast<unsigned>(per) || tile >= tiles) return;   // the whole workgroup
-  const int tok0 = tile % token_tiles * 64, n0 = tile / token_tiles * (COLS * WN) + wn * COLS;
+  const int tall = token_tiles >= 32 ? 8 : 16;   // (4096 tokens x 4096 x 4096: 118.6 us in 16s, 114.7 in 8s; 777 x 4096 x 11008: 76.0 and 78.4)
+  const int band = tile / (tall * col_tiles), in_band = tile - band * tall * col_tiles, high = min(tall, token_tiles - tall * band);
+  const int tok0 = (tall * band + in_band % high) * 64, n0 = in_band / high * (COLS * WN) + wn * COLS;
 
   // this group's stages [s0, s1), of which the last of all may be half a one (k = 64 mod 128): `whole` stages and then that
   const int stages = (a.k + TK - 1) / TK;
@@ -288,8 +291,7 @@ __global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Arg
 
   // weights: row blocks 0..3; SwiGLU: gate rows in 0 and 1, the same rows of up in 2 and 3.  Rows past the end repeat the last.
   // Loads as in the kernel for few tokens, four neighbouring lanes to 64 bytes of a row, but straight to the wave's LDS (two stages);
-  // scales by lane = row, 16 bytes for four stages, and from lane to lane.  (A scale load's wait drains the loads sent before it:
-  // once in four stages.)
+  // scales by lane = row, 16 bytes for four stages, and from lane to lane.
   auto row_of = [&](int rb, int r) __attribute__((always_inline)) -> long long { return min(n0 + 16 * (DUAL ? rb % 2 : rb) + r, a.n - 1); };
   auto resource = [](const void* at, unsigned long long bytes) __attribute__((always_inline)) -> u32x4 {
     const unsigned long long p = reinterpret_cast<unsigned long long>(at);
@@ -384,10 +386,6 @@ __global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Arg
       const int i = q / 4, rb = q % 4;
       __builtin_amdgcn_sched_barrier(0);
       x[(i + 1) % 2][rb] = i < 3 ? read_x(i + 1, rb, slot) : read_x(0, rb, slot1);
-      if (q == 10 && (st1 & 3) == 0 && st1 != st) {
-        scales = scales_next;
-        scales_next = load_scales(min(st1 + 4, s1 - 1));
-      }
       if (q == 10) four = stage_scales(scales, st1);
       if (q >= 11 && q < 15) {
         if (q == 11) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");   // the next stage's codes: all but this stage's loads
@@ -400,6 +398,11 @@ __global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Arg
         asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        // (The wait for this drains what was sent before it: here that is the next stage's codes alone.)
+        if ((st1 & 3) == 0 && st1 != st) {
+          scales = scales_next;
+          scales_next = load_scales(min(st1 + 4, s1 - 1));
+        }
       }
       if (q >= 2 && q < 6) load_x(q - 2, st2, slot2);
       if (q >= 6 && q < 10) load_w(q - 6, st2, HERE);
@@ -513,10 +516,17 @@ int launch_tile(LinearW4Args& a, hipStream_t stream) {
                        WK * (kTileRing * kTileStage + 4 * 2 * kTileCodes));
 }
 
+// Which kernel.  Both take about k times a constant per round of workgroups on the chip's 256 CUs, whatever the round holds: the
+// one for few tokens, 32 rows (SwiGLU 16) x 64 tokens a workgroup, 2.45 us per 1000 of k; the other, 256 rows (128) x 64 tokens, 7.0 us
+// with two groups of waves along k and one workgroup a CU, 12.5 us with one group and two workgroups a CU.  Timed on 100 shapes, n 1024 to
+// 12288, k 1024 to 11008, 40 to 1500 tokens; 4096 x 4096: 128 tokens 13.2 us here, 31.3 there; 512 tokens 43.4 and 32.4.
 template <bool DUAL>
-int launch_many(LinearW4Args& a, hipStream_t stream) {
-  const int64_t tiles = static_cast<int64_t>((a.m + 63) / 64) * ((a.n + (DUAL ? 127 : 255)) / (DUAL ? 128 : 256));
-  return tiles > 256 ? launch_tile<DUAL, 1>(a, stream) : launch_tile<DUAL, 2>(a, stream);
+int launch_any(LinearW4Args& a, hipStream_t stream) {
+  const int64_t token_tiles = (a.m + 63) / 64, tiles = token_tiles * ((a.n + (DUAL ? 127 : 255)) / (DUAL ? 128 : 256));
+  const int64_t few_rounds = (token_tiles * (a.n / (DUAL ? 16 : 32)) + 255) / 256;
+  const double few = 2.45 * static_cast<double>(few_rounds), many = tiles <= 256 ? 7.0 : 12.5 * static_cast<double>((tiles + 511) / 512);
+  if (a.m <= 64 || a.k < 512 || few <= many) return launch_few<DUAL>(a, stream);
+  return tiles <= 256 ? launch_tile<DUAL, 2>(a, stream) : launch_tile<DUAL, 1>(a, stream);
 }
 
 }  // namespace
@@ -534,9 +544,7 @@ int launch_linear_w4(const void* x, const void* w, const void* ws, const void* w
   a.m = static_cast<int>(m);
   a.n = static_cast<int>(n);
   a.k = static_cast<int>(k);
-  const bool dual = w2 != nullptr;
-  if (m <= 64 || k < 512) return dual ? launch_few<true>(a, stream) : launch_few<false>(a, stream);
-  return dual ? launch_many<true>(a, stream) : launch_many<false>(a, stream);
+  return w2 != nullptr ? launch_any<true>(a, stream) : launch_any<false>(a, stream);
 }
 
 }  // namespace kvra

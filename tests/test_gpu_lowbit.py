@@ -280,6 +280,7 @@ def weights(seed, n, k):
 @pytest.mark.parametrize("m,n,k", [
     (1, 32, 64), (1, 96, 192), (2, 160, 128), (15, 64, 320), (16, 256, 1088), (17, 96, 64), (33, 352, 704), (64, 128, 256), (65, 64, 448),
     (100, 1056, 576), (129, 512, 1024), (257, 320, 192), (1, 4096, 4096), (5, 1024, 11008), (300, 1024, 2048), (1, 12288, 4096),
+    (300, 4096, 1088), (390, 4064, 512), (1100, 4128, 576), (1090, 4096, 1024), (2050, 2080, 704),   # 256 rows a workgroup, k shared or not, half stages
 ])
 def test_linear(form, m, n, k):
     x = synth.normal_bf16(14, m, 0, (m, k))
