@@ -330,6 +330,7 @@ extern "C" int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void
   if (!aligned(q) || !aligned(k_cache) || !aligned(v_cache) || !aligned(out)) return KVRA_EINVAL;
   if (workspace_bytes < kvra::attn_q8_workspace_bytes() || !aligned(workspace, 256)) return KVRA_EINVAL;
   if (chunk_len > kMaxTokens || prefix_len > kMaxTokens) return KVRA_EUNSUPPORTED;
+  if (chunk_len * (n_q_heads / n_kv_heads) > (int64_t(1) << 30)) return KVRA_EUNSUPPORTED;
   return kvra::launch_chunk_attn_q8(kvra::Q8Cache{k_cache, v_cache, k_scale, v_scale}, q, prefix_len, chunk_len, n_q_heads,
                                     n_kv_heads, head_dim, scale, out, workspace, static_cast<hipStream_t>(stream));
 }

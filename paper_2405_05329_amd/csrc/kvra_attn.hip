@@ -57,6 +57,7 @@
 // group's free slots can form gangs of one slot per row tile, the tails of a head are run side by side by a
 // gang instead (gang mode, see plan_chunk_attn), so that they share the K/V stream as the heads do.
 #include "kvra_attn_device.h"
+#include "kvra_lowbit_device.h"
 
 #include <algorithm>
 #include <mutex>
@@ -106,6 +107,14 @@ struct AttnArgs {
 #endif
   unsigned fill_seg[kMaxSlots + 1];
   unsigned fill_off[kMaxSlots + 1];
+};
+
+// The same over a cache in 8 bits (kvra_chunk_attn_q8).
+struct AttnQ8Args : AttnArgs {
+  const unsigned char* k8;
+  const unsigned char* v8;
+  const unsigned char* k_scale;
+  const unsigned char* v_scale;
 };
 
 #ifdef KVRA_TRACE
@@ -253,8 +262,14 @@ constexpr int kPartialFloats(int D) { return kWaves * (D / 32 * 16 + 2) * 64; } 
 // un-normalised state (O, m, l per lane) goes to the piece's partial-result slot of group x, and the piece
 // of the unit that gets there last merges all of them (in a fixed order, so that the result does not depend
 // on which one that was) and writes the output.
-template <int D>
-__device__ __forceinline__ void attend(const AttnArgs& a, u32x4* smem, int* last_flag, const int x, const Piece& pc
+//
+// Q8: the cache holds e4m3 with a scale per block of 64 keys and head.  Tiles come as bytes to a small buffer that each wave
+// has for itself (its sixteenth - one load of K, one of V - of the tiles two steps further on than below); in the step in which the bf16 kernel
+// sends for its piece of a tile the wave converts the piece instead, and writes it to the ring slot it would have
+// landed in.  16 conversions, 2 reads and 4 writes of LDS a step more, 2 loads instead of 4, half the bytes; the MFMA block and the schedule are
+// the same, and so are the results, bit for bit, as kvra_chunk_attn's with such a plan on the cache's values.
+template <int D, bool Q8, class Args>
+__device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_flag, const int x, const Piece& pc
 #ifdef KVRA_TRACE
                                        , unsigned long long* trace_rec
 #endif
@@ -355,11 +370,88 @@ __device__ __forceinline__ void attend(const AttnArgs& a, u32x4* smem, int* last
                  uniform(rows * row_bytes), 0x00020000u};
   };
   // tile t of K (or V) -> ring slot dst
-  auto dma_tile = [&](unsigned long long head_base, const unsigned (&off)[LOADS], int t, u32x4* dst) __attribute__((always_inline)) {
+  [[maybe_unused]] auto dma_tile = [&](unsigned long long head_base, const unsigned (&off)[LOADS], int t, u32x4* dst) __attribute__((always_inline)) {
     const u32x4 res = tile_resource(head_base, t);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
       lds_dma16(res, off[i], static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)(dst + (i * kWaves + wave) * 64))));
+  };
+
+  // ---- Q8 ------------------------------------------------------------------------------------
+  // raw: [wave][K, V][parity of the tile] 1 KiB, behind the rings; then a word for each 32 keys of the up to 8 tiles that hold a key hidden
+  // from a row of the workgroup, in which a row of V with a NaN is marked (see stage_v)
+  constexpr int RAW_CPR = D / 16;
+  [[maybe_unused]] const unsigned raw_lds = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV(kStages))) + wave * 4096;
+  [[maybe_unused]] unsigned* const bad_rows = reinterpret_cast<unsigned*>(ldsV(kStages)) + kWaves * 1024;
+  [[maybe_unused]] const int raw_row = (wave * 64 + lane) / RAW_CPR, raw_col = lane % RAW_CPR;
+  [[maybe_unused]] const unsigned raw_off = static_cast<unsigned>(raw_row) * (row_bytes / 2) + raw_col * 16;
+  // where the lane's 16 values go in a bf16 tile: two pieces side by side up to the swizzle, 16 bytes apart one way or the other
+  [[maybe_unused]] const unsigned k_put = static_cast<unsigned>(raw_row * CPR + ((2 * raw_col) ^ ((raw_row / RPB) % CPR))) * 16;
+  [[maybe_unused]] const unsigned v_put = static_cast<unsigned>(raw_row * CPR + ((2 * raw_col) ^ (2 * ((raw_row / RPB) % (CPR / 2))))) * 16;
+  [[maybe_unused]] const int diag0 = (a.prefix + row_lo / a.G + 1) / BN;    // first tile with a key hidden from a row of the workgroup
+  [[maybe_unused]] unsigned scale_bytes = 0;   // lane j % 64: step j's, K's of tile j + phase + 2 and, above it, V's of the one before
+  if constexpr (Q8) {
+    for (int i = tid; i < 32; i += kThreads) bad_rows[i] = 0;
+  }
+  [[maybe_unused]] auto raw_resource = [&](const unsigned char* cache, int t) __attribute__((always_inline)) -> u32x4 {
+    const unsigned long long at = reinterpret_cast<unsigned long long>(cache) + static_cast<unsigned long long>(g) * D +
+                                  static_cast<unsigned long long>(jt0 + t) * (tile_bytes / 2);
+    const int rows = min(max(rows_end - (jt0 + t) * BN, 0), BN);
+    return u32x4{uniform(static_cast<unsigned>(at)), uniform(static_cast<unsigned>(at >> 32) & 0xFFFFu),
+                 uniform(rows > 0 ? rows * (row_bytes / 2) - g * D : 0u), 0x00020000u};
+  };
+  // sends for the bytes of K tile t and V tile t - 1
+  [[maybe_unused]] auto send_raw = [&](int t) __attribute__((always_inline)) {
+    if constexpr (Q8) {
+      lds_dma16(raw_resource(a.k8, t), raw_off, uniform(raw_lds + (t & 1) * 1024));
+      lds_dma16(raw_resource(a.v8, t - 1), raw_off, uniform(raw_lds + 2048 + ((t - 1) & 1) * 1024));
+    }
+  };
+  [[maybe_unused]] auto block_of = [&](int t) __attribute__((always_inline)) -> long long {   // of this wave's rows of tile t
+    return static_cast<long long>(jt0 + t) * (BN / 64) + wave * (64 / RAW_CPR) / 64;
+  };
+  [[maybe_unused]] auto load_scale_bytes = [&](int step) __attribute__((always_inline)) {   // of steps step ..
+    if constexpr (Q8) {
+      const long long kb = block_of(step + lane + phase + 2), vb = block_of(step + lane + phase + 1), end = (static_cast<long long>(rows_end) + 63) / 64;
+      const unsigned ks = kb < end ? a.k_scale[kb * a.Hkv + g] : 127u, vs = vb < end ? a.v_scale[vb * a.Hkv + g] : 127u;
+      scale_bytes = ks | vs << 8;
+    }
+  };
+  [[maybe_unused]] auto factors = [&](int j, float* kf, float* vf) __attribute__((always_inline)) {
+    if (j != 0 && (j & 63) == 0) load_scale_bytes(j);
+    const unsigned both = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(scale_bytes), j & 63));
+    *kf = scale_factor(both & 255u);
+    *vf = scale_factor(both >> 8);
+  };
+  // 16 codes -> bf16, to place `put` of the tile at LDS byte address tile
+  [[maybe_unused]] auto put_values = [&](u32x4 codes, float factor, unsigned tile, unsigned put) __attribute__((always_inline)) {
+    u32x4 w[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i / 2][2 * (i % 2)] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], factor, false));
+      w[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], factor, true));
+    }
+    *(lds_u32x4*)static_cast<uintptr_t>(tile + put) = w[0];
+    *(lds_u32x4*)static_cast<uintptr_t>(tile + (put ^ 16u)) = w[1];
+  };
+  // A NaN in a row of V must not reach the rows it is hidden from (a weight of zero times NaN), nor be lost for those that see
+  // it: in tiles that hold keys hidden from a row of the workgroup it becomes a zero, and its key is marked; the scores of
+  // a marked key are NaN.
+  [[maybe_unused]] auto without_nan = [&](u32x4 codes, int t) __attribute__((always_inline)) -> u32x4 {
+    if (jt0 + t >= diag0) {
+      unsigned bad = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad |= nan_bytes(codes[i]);
+      if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes[i] &= ~((nan_bytes(codes[i]) >> 7) * 255u);
+        if (bad != 0) atomicOr(bad_rows + (jt0 + t - diag0) * 4 + raw_row / 32, 1u << (raw_row % 32));
+      }
+    }
+    return codes;
+  };
+  [[maybe_unused]] auto raw_at = [&](unsigned addr) __attribute__((always_inline)) -> u32x4 {
+    return *(lds_u32x4*)static_cast<uintptr_t>(addr + lane * 16);
   };
 
   f32x4 o[DB][QB];
@@ -410,17 +502,42 @@ __device__ __forceinline__ void attend(const AttnArgs& a, u32x4* smem, int* last
   unsigned slot_k[kStages], slot_v[kStages];
 #pragma unroll
   for (int r = 0; r < kStages; ++r) {
-    slot_k[r] = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)(ldsK((r + 2 + phase) % kStages) + wave * 64)));
-    slot_v[r] = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)(ldsV((r + 1 + phase) % kStages) + wave * 64)));
+    slot_k[r] = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)(ldsK((r + 2 + phase) % kStages) + (Q8 ? 0 : wave * 64))));
+    slot_v[r] = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)(ldsV((r + 1 + phase) % kStages) + (Q8 ? 0 : wave * 64))));
   }
 
   // ---- prologue: K tiles 0..2 and V tiles 0..1 on their way into LDS -----------------------------
   // the first MFMA block multiplies a zero P by the ring slot "before" V tile 0: make it finite
   for (int i = tid; i < TILE; i += kThreads) ldsV(kStages - 1)[i] = u32x4{0u, 0u, 0u, 0u};
+  if constexpr (Q8) {
+    __syncthreads();                       // the marks are cleared
+    u32x4 raw[5];
+    unsigned scale[5];
 #pragma unroll
-  for (int t = 0; t < 3; ++t) dma_tile(kbase, koff, t, ldsK(t));
+    for (int i = 0; i < 5; ++i) {          // K tiles 0..2, V tiles 0 and 1
+      const int t = i < 3 ? i : i - 3, row = (jt0 + t) * BN + raw_row;
+      const unsigned char* cache = i < 3 ? a.k8 : a.v8;
+      raw[i] = u32x4{0u, 0u, 0u, 0u};
+      scale[i] = 127;
+      if (row < rows_end) {
+        raw[i] = *reinterpret_cast<const u32x4*>(cache + (static_cast<long long>(row) * a.Hkv + g) * D + raw_col * 16);
+        scale[i] = (i < 3 ? a.k_scale : a.v_scale)[static_cast<long long>(row / 64) * a.Hkv + g];
+      }
+    }
 #pragma unroll
-  for (int t = 0; t < 2; ++t) dma_tile(vbase, voff, t, ldsV(t));
+    for (int i = 0; i < 5; ++i) {
+      if (i < 3) put_values(raw[i], scale_factor(scale[i]), static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsK(i))), k_put);
+      else put_values(without_nan(raw[i], i - 3), scale_factor(scale[i]), static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV(i - 3))), v_put);
+    }
+    load_scale_bytes(0);
+    send_raw(phase + 2);
+    send_raw(phase + 3);
+  } else {
+#pragma unroll
+    for (int t = 0; t < 3; ++t) dma_tile(kbase, koff, t, ldsK(t));
+#pragma unroll
+    for (int t = 0; t < 2; ++t) dma_tile(vbase, voff, t, ldsV(t));
+  }
   // every load so far (the Q fragment included) is drained here: a load left pending across the
   // loop entry would make the compiler guard the loop's MFMAs with vmcnt waits
   __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
@@ -500,16 +617,44 @@ __device__ __forceinline__ void attend(const AttnArgs& a, u32x4* smem, int* last
     const int st = j + phase;
     // (handed out one at a time between the exponentials; what does not exist is "loaded" as zeros: no branch, no
     // bookkeeping - every instruction of this block, scalar ones too, is time the matrix pipe waits for)
-    const u32x4 k_res = tile_resource(kbase, st + 2), v_res = tile_resource(vbase, st + 1);
+    const u32x4 k_res = Q8 ? u32x4{} : tile_resource(kbase, st + 2), v_res = Q8 ? u32x4{} : tile_resource(vbase, st + 1);
+    [[maybe_unused]] float k_factor = 1.0f, v_factor = 1.0f;
+    [[maybe_unused]] u32x4 raw;
+    if constexpr (Q8) {
+      factors(j, &k_factor, &v_factor);
+      asm volatile("s_waitcnt vmcnt(2)" ::: "memory");   // the bytes of K tile st + 2 and V tile st + 1: all but the last two loads
+    }
     auto stage_piece = [&](int idx) __attribute__((always_inline)) {
       __builtin_amdgcn_sched_barrier(0);
-      if (idx < LOADS)
+      if constexpr (Q8) {
+        if (idx == 0) raw = raw_at(raw_lds + (st & 1) * 1024);
+        else if (idx == 1) put_values(raw, k_factor, slot_k[RS], k_put);
+        else if (idx == 2) raw = raw_at(raw_lds + 2048 + ((st + 1) & 1) * 1024);
+        else put_values(without_nan(raw, st + 1), v_factor, slot_v[RS], v_put);
+      } else if (idx < LOADS)
         lds_dma16(k_res, koff[idx], slot_k[RS] + idx * (kWaves * 64 * 16));
       else
         lds_dma16(v_res, voff[idx - LOADS], slot_v[RS] + (idx - LOADS) * (kWaves * 64 * 16));
       __builtin_amdgcn_sched_barrier(0);
     };
     {
+      if constexpr (Q8) {
+        if (jt0 + j >= diag0) {
+#pragma unroll
+          for (int w = 0; w < BN / 32; ++w) {
+            const unsigned marks = uniform(bad_rows[(jt0 + j - diag0) * 4 + w]);
+            if (__builtin_expect(marks != 0, 0)) {
+#pragma unroll
+              for (int kb = 2 * w; kb < 2 * w + 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (marks >> (16 * (kb % 2) + 4 * g4 + e) & 1u)
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) s[kb][qb][e] = __builtin_nanf("");
+            }
+          }
+        }
+      }
       // register e of block (kb, qb) is key  j*BN + 16 kb + 4 g4 + e  of query 16 qb + n
       if ((jt0 + j) * BN + BN - 1 > wmin) {
         const float ninf = -INFINITY;
@@ -607,7 +752,8 @@ __device__ __forceinline__ void attend(const AttnArgs& a, u32x4* smem, int* last
       for (int qb = 0; qb < QB; ++qb) l[qb] += psum[qb][0] + psum[qb][1];
     }
     // everything issued before this block (tiles K(st+1), V(st)) must have landed before the barrier
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * LOADS));
+    if constexpr (Q8) send_raw(st + 4);
+    else __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * LOADS));
     if (!ONE_BARRIER || phase == 0) __syncthreads();
   };
   for (int j0 = 0; j0 < jw; j0 += kStages) {
@@ -630,6 +776,17 @@ __device__ __forceinline__ void attend(const AttnArgs& a, u32x4* smem, int* last
   for (int j = jw; j <= nt; ++j) {
     if (!ONE_BARRIER || phase == 1) __syncthreads();
     const int st = j + phase;
+    if constexpr (Q8) {
+      float kf, vf;
+      factors(j, &kf, &vf);
+      asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+      put_values(raw_at(raw_lds + (st & 1) * 1024), kf, static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsK((st + 2) % kStages))), k_put);
+      put_values(without_nan(raw_at(raw_lds + 2048 + ((st + 1) & 1) * 1024), st + 1), vf,
+                 static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV((st + 1) % kStages))), v_put);
+      send_raw(st + 4);
+      if (!ONE_BARRIER || phase == 0) __syncthreads();
+      continue;
+    }
     // (Nothing is sent for tiles that do not exist, so that the last waits are for data alone: 0.1 to 0.3 us a launch.)
     if (st + 2 < nt) {
       dma_tile(kbase, koff, st + 2, ldsK((st + 2) % kStages));
@@ -827,7 +984,7 @@ __global__ __launch_bounds__(kThreads, 1) void chunk_attn_kernel(AttnArgs a) {
         ? a.trace + (static_cast<long long>(blockIdx.x) * kTracePieces + ordinal) * kTraceWords : nullptr;
     ++ordinal;
     KVRA_TRACE_STAMP(rec, 0);
-    attend<D>(a, smem, &last_flag, x, pc, rec);
+    attend<D, false>(a, smem, &last_flag, x, pc, rec);
     KVRA_TRACE_STAMP(rec, 3);
     if (rec != nullptr && threadIdx.x == 0) {
       unsigned hw, xcc;
@@ -841,7 +998,23 @@ __global__ __launch_bounds__(kThreads, 1) void chunk_attn_kernel(AttnArgs a) {
       rec[7] = (static_cast<unsigned long long>(static_cast<unsigned>(pc.slot + 1)) << 32) | static_cast<unsigned>(pc.jt0);
     }
 #else
-    attend<D>(a, smem, &last_flag, x, pc);
+    attend<D, false>(a, smem, &last_flag, x, pc);
+#endif
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 1) void chunk_attn_q8_kernel(AttnQ8Args a) {
+  extern __shared__ u32x4 smem[];
+  __shared__ int last_flag;
+  const int x = blockIdx.x % a.groups, c = blockIdx.x / a.groups;
+  PieceWalker walker(a, x, c);
+  Piece pc;
+  while (walker.next(a, &pc)) {
+#ifdef KVRA_TRACE
+    attend<D, true>(a, smem, &last_flag, x, pc, nullptr);
+#else
+    attend<D, true>(a, smem, &last_flag, x, pc);
 #endif
   }
 }
@@ -1330,6 +1503,28 @@ int rows_splits(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int
 
 }  // namespace
 
+namespace {
+
+// The same choice over a cache in 8 bits: rows of a slice of the kernel for few rows and workgroups for each, or *splits = 0.
+void rows_q8_shape(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus,
+                   int* rows, int* splits) {
+  const int64_t vrows = chunk_len * (n_q_heads / n_kv_heads);
+  *rows = vrows <= 16 ? 16 : 32;
+  *splits = 0;
+  const int64_t units = (vrows + *rows - 1) / *rows * n_kv_heads, tiles = (prefix_len + chunk_len + 63) / 64;
+#ifdef KVRA_Q8_FORCE
+  if (KVRA_Q8_FORCE == 2) return;
+#else
+  if (rows_splits(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, kStaticSlots * attn_partial_bytes(128)) == 0) return;
+#endif
+  // as many workgroups per slice as leave one per CU, none without a key tile for each of its waves
+  int64_t s = 1;
+  if (units <= kCounterInts) s = std::max<int64_t>(1, std::min(std::min<int64_t>(cus / units, (tiles + 7) / 8), int64_t(32)));
+  *splits = static_cast<int>(s);
+}
+
+}  // namespace
+
 int attn_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus, int* splits) {
   AttnPlan plan;
   const int rc = plan_chunk_attn(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, true, &plan);
@@ -1394,6 +1589,55 @@ int launch_chunk_attn(const AttnLaunch& l, const void* q, const void* k_cache, c
   const dim3 g_main(static_cast<unsigned>(workgroups));
   return head_dim == 128 ? launch_kernel(chunk_attn_kernel<128>, g_main, b3, a, stream, smem)
                          : launch_kernel(chunk_attn_kernel<64>, g_main, b3, a, stream, smem);
+}
+
+// ---- over a cache in 8 bits --------------------------------------------------------------------
+// The workspace is the caller's: merge counters, then the partial-result slots (of the tiled kernel, or of the one for few rows).
+namespace {
+
+constexpr int kQ8Counters = 4096;
+static_assert(kQ8Counters >= kCounterInts, "");
+
+}  // namespace
+
+int64_t attn_q8_workspace_bytes() { return (kQ8Counters * int64_t(4) + kStaticSlots * attn_partial_bytes(128) + 4095) / 4096 * 4096; }
+
+int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
+                         int head_dim, float scale, void* out, void* workspace, hipStream_t stream) {
+  const int cus = current_device_cus();
+  if (cus < 1) return KVRA_ENODEVICE;
+  AttnPlan plan;
+  int rc = cached_plan(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, true, &plan);
+  if (rc == KVRA_OK && plan.scratch_slots > kStaticSlots)   // (a device with more than 256 CUs)
+    rc = cached_plan(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, false, &plan);
+  if (rc != KVRA_OK) return rc;
+  int* const counters = static_cast<int*>(workspace);
+  float* const partial = reinterpret_cast<float*>(counters + kQ8Counters);
+  int rows = 0, splits = 0;
+  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, &rows, &splits);
+  if (splits > 0)
+    return launch_attn_rows_q8(cache, q, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, scale, out, rows, splits, partial,
+                               counters, stream);
+  AttnQ8Args a;
+  schedule_args(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, &a);
+  a.q = static_cast<const __bf16*>(q);
+  a.k = nullptr;
+  a.v = nullptr;
+  a.out = static_cast<__bf16*>(out);
+  a.c_log2 = scale * 1.4426950408889634f;
+  a.scratch = partial;
+  a.counters = counters;
+#ifdef KVRA_TRACE
+  a.trace = nullptr;
+#endif
+  a.k8 = static_cast<const unsigned char*>(cache.k);
+  a.v8 = static_cast<const unsigned char*>(cache.v);
+  a.k_scale = static_cast<const unsigned char*>(cache.k_scale);
+  a.v_scale = static_cast<const unsigned char*>(cache.v_scale);
+  const unsigned smem = 2u * kStages * static_cast<unsigned>(a.bn) * static_cast<unsigned>(head_dim) * 2u + kWaves * 4096u + 128u;   // rings, bytes, marks
+  const dim3 grid(static_cast<unsigned>(plan.groups * plan.slots)), block(kThreads);
+  return head_dim == 128 ? launch_kernel(chunk_attn_q8_kernel<128>, grid, block, a, stream, smem)
+                         : launch_kernel(chunk_attn_q8_kernel<64>, grid, block, a, stream, smem);
 }
 
 }  // namespace kvra

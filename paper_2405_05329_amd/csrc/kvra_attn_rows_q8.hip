@@ -25,7 +25,6 @@ constexpr int kQ8Threads = 64 * kQ8Waves;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 struct RowsQ8Args {
@@ -444,29 +443,6 @@ int launch_attn_rows_q8(const Q8Cache& cache, const void* q, int64_t prefix_len,
                       : launch_kernel(attn_rows_q8_kernel<128, 2>, grid, block, a, stream, smem);
   return rows == 16 ? launch_kernel(attn_rows_q8_kernel<64, 1>, grid, block, a, stream, smem)
                     : launch_kernel(attn_rows_q8_kernel<64, 2>, grid, block, a, stream, smem);
-}
-
-// The workspace: counters, then partial results.
-constexpr int kQ8Counters = 4096;
-constexpr int64_t kQ8WorkspaceBytes = int64_t(100) << 20;
-
-int64_t attn_q8_workspace_bytes() { return kQ8WorkspaceBytes; }
-
-int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
-                         int head_dim, float scale, void* out, void* workspace, hipStream_t stream) {
-  const int G = n_q_heads / n_kv_heads;
-  const int64_t vrows = chunk_len * G;
-  if (vrows > (int64_t(1) << 30)) return KVRA_EUNSUPPORTED;
-  const int cus = current_device_cus();
-  if (cus < 1) return KVRA_ENODEVICE;
-  const int rows = vrows <= 16 ? 16 : 32;
-  const int64_t units = (vrows + rows - 1) / rows * n_kv_heads, tiles = (prefix_len + chunk_len + 63) / 64;
-  // as many workgroups per slice as leave one per CU, none without a key tile for each of its waves
-  int64_t splits = 1;
-  if (units <= kQ8Counters) splits = std::max<int64_t>(1, std::min(std::min<int64_t>(cus / units, (tiles + 7) / 8), int64_t(32)));
-  int* const counters = static_cast<int*>(workspace);
-  return launch_attn_rows_q8(cache, q, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, scale, out, rows, static_cast<int>(splits),
-                             reinterpret_cast<float*>(counters + kQ8Counters), counters, stream);
 }
 
 }  // namespace kvra

@@ -265,7 +265,6 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
 constexpr int kTileStage = 64 * 256;      // bytes: 64 tokens x 128 of k
 constexpr int kTileRing = 3;
 constexpr int kTileCodes = 64 * 64;       // of a wave: 64 rows x 128 of k
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4_w4;
 
 template <bool DUAL, int WK>
 __global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Args a) {
@@ -309,7 +308,7 @@ __global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Arg
   };
   const unsigned w_addr = lds_w + r16 * 64 + (g4 ^ (-(r16 >> 2) & 3)) * 16;
   auto read_w = [&](int rb, unsigned half) __attribute__((always_inline)) -> u32x4 {
-    return *(lds_u32x4_w4*)static_cast<uintptr_t>(w_addr + half + rb * 1024);
+    return *(lds_u32x4*)static_cast<uintptr_t>(w_addr + half + rb * 1024);
   };
   const unsigned char* const s_row = (DUAL && lane >= 32 ? a.ws2 : a.ws) + row_of(lane >> 4, r16) * (a.k / 32);
   u32x4 scales, scales_next;
