@@ -1517,9 +1517,9 @@ void rows_q8_shape(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, 
 #else
   if (rows_splits(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, kStaticSlots * attn_partial_bytes(128)) == 0) return;
 #endif
-  // as many workgroups per slice as leave one per CU, none without a key tile for each of its waves
+  // as many workgroups per slice as leave one per CU, none without two key tiles for each of its waves
   int64_t s = 1;
-  if (units <= kCounterInts) s = std::max<int64_t>(1, std::min(std::min<int64_t>(cus / units, (tiles + 7) / 8), int64_t(32)));
+  if (units <= kCounterInts) s = std::max<int64_t>(1, std::min(std::min<int64_t>(cus / units, (tiles + 15) / 16), int64_t(32)));
   *splits = static_cast<int>(s);
 }
 

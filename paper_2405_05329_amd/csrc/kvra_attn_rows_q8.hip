@@ -41,7 +41,6 @@ struct RowsQ8Args {
   int G;
   int slices;        // slices of 16 QB virtual rows per kv head
   int splits;        // workgroups that share the key tiles of a slice
-  int by_xcd;        // Hkv * splits is a multiple of 8: the slices of a (head, split) pair share an XCD
   float c_log2;      // scale * log2(e)
   float* partial;    // splits > 1: rows_q8_slot_floats(D, QB) per workgroup
   int* counters;     // splits > 1: pieces counted so far, one per slice; all zero between launches
@@ -76,26 +75,20 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // wave-uniform by construction
   const int n = lane & 15, g4 = lane >> 4;
 
-  // workgroup -> (kv head, split, slice); ids go round-robin over the 8 XCDs.  Last slices first: they see the most keys.
-  int pair, slice;
-  if (a.by_xcd) {
-    const int rest = blockIdx.x >> 3;
-    slice = a.slices - 1 - rest % a.slices;
-    pair = (blockIdx.x & 7) + 8 * (rest / a.slices);
-  } else {
-    const int pairs = a.Hkv * a.splits;
-    slice = a.slices - 1 - blockIdx.x / pairs;
-    pair = blockIdx.x % pairs;
-  }
-  const int g = pair / a.splits, split = pair - g * a.splits;
+  // grid (kv heads, splits, slices), so that nothing has to be divided; ids go round-robin over the 8 XCDs, which so read apart by
+  // head (27 against 29.5 us for the bytes of 16384 x 32 x 128 alone).  Last slices first: they see the most keys.
+  const int g = blockIdx.x, split = blockIdx.y, slice = a.slices - 1 - static_cast<int>(blockIdx.z);
 
   const int VR = a.chunk * a.G, total = a.prefix + a.chunk;
   const int v0 = slice * ROWS, row_hi = min(v0 + ROWS, VR);
-  const int wmin = a.prefix + v0 / a.G;                 // last visible key of the slice's first and last row
-  const int wmax = a.prefix + (row_hi - 1) / a.G;
+  // (a division is some 20 instructions, and a step of one token waits for each of them)
+  auto token_of = [&](int vr) __attribute__((always_inline)) -> int { return a.chunk == 1 ? 0 : static_cast<int>(static_cast<unsigned>(vr) / static_cast<unsigned>(a.G)); };
+  const int wmin = a.prefix + token_of(v0);             // last visible key of the slice's first and last row
+  const int wmax = a.prefix + token_of(row_hi - 1);
   const int tiles = wmax / BN + 1;
-  const int t_lo = static_cast<int>(static_cast<long long>(tiles) * split / a.splits);
-  const int t_hi = static_cast<int>(static_cast<long long>(tiles) * (split + 1) / a.splits);
+  // (at most 2^19 tiles and 32 splits)
+  const int t_lo = a.splits == 1 ? 0 : static_cast<int>(static_cast<unsigned>(tiles * split) / static_cast<unsigned>(a.splits));
+  const int t_hi = a.splits == 1 ? tiles : static_cast<int>(static_cast<unsigned>(tiles * (split + 1)) / static_cast<unsigned>(a.splits));
 
   // Piece p = 64 i + lane of a tile = (row p / CPR, slot p % CPR); the lane that owns slot (row, slot) fetches column piece
   // slot ^ f(row), so that the reads below are free of bank conflicts: K is read 16 bytes a lane down 16 rows of one column
@@ -141,9 +134,9 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
 
   int t = t_lo + wave;
   if (t < t_hi) {
-    load_scales(t);
     load_tile(a.k, t, lds_k, k_xor);
     load_tile(a.v, t, lds_v, v_xor);
+    load_scales(t);
   }
 
   // Q fragments: B operand of S^T.  The lanes of a 16-lane row g take pieces g and g + 4 of a key's row, so contraction
@@ -152,7 +145,7 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
   int qpos[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const int vr = min(v0 + 16 * qb + n, row_hi - 1), r = vr / a.G, h = g * a.G + (vr - r * a.G);
+    const int vr = min(v0 + 16 * qb + n, row_hi - 1), r = token_of(vr), h = g * a.G + (vr - r * a.G);
     qpos[qb] = a.prefix + r;
     const __bf16* qrow = a.q + (static_cast<long long>(r) * a.H + h) * D;
 #pragma unroll
@@ -341,15 +334,18 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
   if (a.splits > 1) {
     // device-coherent stores, acknowledged before the piece is counted; the piece that completes the count merges all of
     // them in their order, so the result does not depend on which one that is
-    const int unit = g * a.slices + slice;
+    const int unit = g * a.slices + slice, live = row_hi - v0;   // (rows that are not there are neither stored nor merged)
     constexpr int SLOT = rows_q8_slot_floats(D, QB);
     float* const slots = a.partial + static_cast<long long>(unit) * a.splits * SLOT;
     float* const mine = slots + static_cast<long long>(split) * SLOT;
 #pragma unroll
-    for (int i = 0; i < RW; ++i) store_coherent(mine + (r0 + i) * 64 + lane, acc[i]);
+    for (int j = 0; j < QW; ++j)
+      if (16 * (qb0 + j) + n < live)
+#pragma unroll
+        for (int i = 0; i < RE; ++i) store_coherent(mine + (r0 + RE * j + i) * 64 + lane, acc[RE * j + i]);
 #pragma unroll
     for (int j = 0; j < QW; ++j)
-      if (r0 < 4 * QB && g4 == 0) {         // the waves that hold the first of a query block's registers write its m and l
+      if (r0 < 4 * QB && g4 == 0 && 16 * (qb0 + j) + n < live) {         // the waves that hold the first of a query block's registers write its m and l
         store_coherent(mine + R * 64 + 16 * (qb0 + j) + n, am[j]);
         store_coherent(mine + R * 64 + ROWS + 16 * (qb0 + j) + n, al[j]);
       }
@@ -366,7 +362,9 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
     }
 #pragma unroll
     for (int i = 0; i < RW; ++i) acc[i] = 0.0f;
+    if (16 * qb0 + n >= live) return;       // (no barrier from here on)
     constexpr int AHEAD = 8;                // partial results on their way together
+#pragma unroll 1
     for (int p0 = 0; p0 < a.splits; p0 += AHEAD) {
       float pv[AHEAD][RW], pm[AHEAD][QW], pl[AHEAD][QW];
 #pragma unroll
@@ -382,11 +380,11 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        if (p0 + u >= a.splits) break;
 #pragma unroll
         for (int j = 0; j < QW; ++j) {
-          const float mn = fmaxf(am[j], pm[u][j]);
-          const float wa = __builtin_amdgcn_exp2f(am[j] - mn), wb = __builtin_amdgcn_exp2f(pm[u][j] - mn);
+          const bool there = p0 + u < a.splits;   // (past the last it is loaded again, and weighs nothing)
+          const float mn = there ? fmaxf(am[j], pm[u][j]) : am[j];
+          const float wa = __builtin_amdgcn_exp2f(am[j] - mn), wb = there ? __builtin_amdgcn_exp2f(pm[u][j] - mn) : 0.0f;
           am[j] = mn;
           al[j] = fmaf(pl[u][j], wb, al[j] * wa);
 #pragma unroll
@@ -402,7 +400,7 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
   for (int j = 0; j < QW; ++j) {
     const int vr = v0 + 16 * (qb0 + j) + n, db = r0 / (4 * QB), e0 = r0 % 4;
     if (vr >= row_hi) continue;
-    const int r = vr / a.G, h = g * a.G + (vr - r * a.G);
+    const int r = token_of(vr), h = g * a.G + (vr - r * a.G);
     const float inv = 1.0f / al[j];
     out_t w;
 #pragma unroll
@@ -430,13 +428,11 @@ int launch_attn_rows_q8(const Q8Cache& cache, const void* q, int64_t prefix_len,
   a.G = n_q_heads / n_kv_heads;
   a.slices = static_cast<int>((chunk_len * a.G + rows - 1) / rows);
   a.splits = splits;
-  a.by_xcd = n_kv_heads * splits % 8 == 0 ? 1 : 0;
   a.c_log2 = scale * 1.4426950408889634f;
   a.partial = partial;
   a.counters = counters;
-  const int64_t groups = static_cast<int64_t>(a.slices) * n_kv_heads * splits;
-  if (groups > INT32_MAX) return KVRA_EUNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(groups)), block(kQ8Threads);
+  if (a.slices > 65535) return KVRA_EUNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(n_kv_heads), static_cast<unsigned>(splits), static_cast<unsigned>(a.slices)), block(kQ8Threads);
   const unsigned smem = kQ8Waves * (2 * 64 * static_cast<unsigned>(head_dim) + 8u * static_cast<unsigned>(rows)) + 16u;   // tiles, m and l, flag
   if (head_dim == 128)
     return rows == 16 ? launch_kernel(attn_rows_q8_kernel<128, 1>, grid, block, a, stream, smem)
