@@ -49,13 +49,16 @@ __device__ __forceinline__ unsigned short round_bf16(float x) {
   return __builtin_bit_cast(unsigned short, b);
 }
 
-// x in fp32, rounded to odd: what is not exact gets the neighbour whose last bit is 1, on which no later tie can fall.
+// x in fp32, rounded to odd: cut to 24 bits, the last of which also stands for everything cut off, so that no later tie can
+// fall on it.  In integers (fp64 instructions are slow): the bits from the exponent on are x's, moved by 29, its bias by 896.
 __device__ __forceinline__ float round_odd(double x) {
-  const float f = static_cast<float>(x);
-  unsigned u = __float_as_uint(f);
-  const double back = static_cast<double>(f);
-  if (back != x && !(u & 1u) && x == x) u += fabs(back) < fabs(x) ? 1u : ~0u;
-  return __uint_as_float(u);
+  const unsigned long long bits = __builtin_bit_cast(unsigned long long, x);
+  const unsigned lo = static_cast<unsigned>(bits), hi = static_cast<unsigned>(bits >> 32), mag = hi & 0x7FFFFFFFu;
+  unsigned u = __builtin_amdgcn_alignbit(hi, lo, 29) + 0x40000000u;
+  u |= min(lo & 0x1FFFFFFFu, 1u);
+  if (mag - 0x38100000u >= 0x47F00000u - 0x38100000u)   // outside fp32's normal numbers: below them zero, above the largest, or not finite
+    u = mag < 0x38100000u ? 0u : mag < 0x7FF00000u ? 0x7F7FFFFFu : 0x7FC00000u;
+  return __uint_as_float(u | (hi & 0x80000000u));
 }
 
 __device__ __forceinline__ float finite_abs(float x) {
@@ -68,9 +71,13 @@ __device__ __forceinline__ unsigned pack4(float a, float b, float c, float d) {
   return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
 
-__device__ __forceinline__ u32x2 pack8(const float (&x)[16], int at, float factor) {
-  return u32x2{pack4(x[at] * factor, x[at + 1] * factor, x[at + 2] * factor, x[at + 3] * factor),
-               pack4(x[at + 4] * factor, x[at + 5] * factor, x[at + 6] * factor, x[at + 7] * factor)};
+__device__ __forceinline__ u32x2 pack8(const float* x, float factor) {
+  return u32x2{pack4(x[0] * factor, x[1] * factor, x[2] * factor, x[3] * factor), pack4(x[4] * factor, x[5] * factor, x[6] * factor, x[7] * factor)};
+}
+
+__device__ __forceinline__ u32x2 pack8(const u16x8& b, float factor) {
+  const float x[8] = {widen(b[0]), widen(b[1]), widen(b[2]), widen(b[3]), widen(b[4]), widen(b[5]), widen(b[6]), widen(b[7])};
+  return pack8(x, factor);
 }
 
 __device__ __forceinline__ unsigned rescale4(unsigned codes, float factor) {
@@ -123,39 +130,77 @@ __global__ __launch_bounds__(4 * D) void append_q8_kernel(AppendQ8Args a) {
   const int t = tid / UNITS, j = tid % UNITS;
   const bool fresh = t >= held && t < end;
 
+  // A head's rows of the block, and the scales found: on their way while the angles, or the head before, are worked on.
+  struct Rows {
+    u16x8 lo, hi, v0, v1;
+    int k_old, v_old;
+  };
+  auto load = [&](int h) __attribute__((always_inline)) -> Rows {
+    Rows r;
+    r.k_old = r.v_old = kScaleMin + 127;
+    r.lo = r.hi = r.v0 = r.v1 = u16x8{};
+    if (fresh) {
+      const long long in_row = ((first + t - a.prefix_len) * a.n_kv_heads + h) * D;
+      r.lo = *reinterpret_cast<const u16x8*>(a.k_in + in_row + 8 * j);
+      r.hi = *reinterpret_cast<const u16x8*>(a.k_in + in_row + HALF + 8 * j);
+      r.v0 = *reinterpret_cast<const u16x8*>(a.v_in + in_row + 16 * j);
+      r.v1 = *reinterpret_cast<const u16x8*>(a.v_in + in_row + 16 * j + 8);
+    }
+    if (held > 0) {
+      const long long scale_at = (first / 64) * a.n_kv_heads + h;
+      r.k_old = a.k_scale[scale_at];
+      r.v_old = a.v_scale[scale_at];
+    }
+    return r;
+  };
+  Rows now = load(h0);
+
   double c8[8], s8[8];
   if (a.use_rope) {
     const int row = tid / HALF, f = tid % HALF;
     const double freq = a.inv_freq[f];
-#pragma unroll
-    for (int set = 0; set < 2; ++set) {
-      const double phi = (set == 0 ? static_cast<double>(first + 8 * row) : static_cast<double>(row)) * freq;
+    auto angle = [&](double position, int set) __attribute__((always_inline)) {
+      const double phi = position * freq;
       double s, c;
       if (phi < 67108864.0) sincos_reduced(phi, &s, &c);
       else sincos(phi, &s, &c);
       cos_s[set][row][f] = c;
       sin_s[set][row][f] = s;
-    }
-    __syncthreads();
+    };
+    if (end - held <= 8) {                       // (a step's one token, a few: an angle each is all there is)
+      angle(static_cast<double>(first + held + row), 0);
+      __syncthreads();
+      if (fresh) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const double ca = cos_s[0][t / 8][8 * j + e], sa = sin_s[0][t / 8][8 * j + e], cb = cos_s[1][t % 8][8 * j + e], sb = sin_s[1][t % 8][8 * j + e];
-      c8[e] = fma(ca, cb, -(sa * sb));
-      s8[e] = fma(sa, cb, ca * sb);
+        for (int e = 0; e < 8; ++e) {
+          c8[e] = cos_s[0][t - held][8 * j + e];
+          s8[e] = sin_s[0][t - held][8 * j + e];
+        }
+      }
+    } else {
+      angle(static_cast<double>(first + 8 * row), 0);
+      angle(static_cast<double>(row), 1);
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double ca = cos_s[0][t / 8][8 * j + e], sa = sin_s[0][t / 8][8 * j + e], cb = cos_s[1][t % 8][8 * j + e], sb = sin_s[1][t % 8][8 * j + e];
+        c8[e] = fma(ca, cb, -(sa * sb));
+        s8[e] = fma(sa, cb, ca * sb);
+      }
     }
   }
 
   for (int h = h0; h < h1; ++h) {
-    const long long in_row = ((first + t - a.prefix_len) * a.n_kv_heads + h) * D, row = ((first + t) * a.n_kv_heads + h) * D;
+    const long long row = ((first + t) * a.n_kv_heads + h) * D;
     const long long scale_at = (first / 64) * a.n_kv_heads + h;
-    float k[16], v[16];
+    const u16x8 v0 = now.v0, v1 = now.v1;
+    float k[16];
     float kmax = 0.0f, vmax = 0.0f;
+    const int k_old = now.k_old - 127, v_old = now.v_old - 127;
     if (fresh) {
-      const u16x8 lo = *reinterpret_cast<const u16x8*>(a.k_in + in_row + 8 * j), hi = *reinterpret_cast<const u16x8*>(a.k_in + in_row + HALF + 8 * j);
-      const u16x8 v0 = *reinterpret_cast<const u16x8*>(a.v_in + in_row + 16 * j), v1 = *reinterpret_cast<const u16x8*>(a.v_in + in_row + 16 * j + 8);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x0 = widen(lo[e]), x1 = widen(hi[e]);
+        const float x0 = widen(now.lo[e]), x1 = widen(now.hi[e]);
         k[e] = x0;
         k[8 + e] = x1;
         if (a.use_rope) {
@@ -163,20 +208,19 @@ __global__ __launch_bounds__(4 * D) void append_q8_kernel(AppendQ8Args a) {
           k[e] = round_odd(fma(d0, c8[e], -(d1 * s8[e])));
           k[8 + e] = round_odd(fma(d1, c8[e], d0 * s8[e]));
         }
-        v[e] = widen(v0[e]);
-        v[8 + e] = widen(v1[e]);
+        kmax = fmaxf(kmax, fmaxf(fabsf(k[e]), fabsf(k[8 + e])));      // (fmaxf takes the number beside a NaN)
+        vmax = fmaxf(vmax, fmaxf(fabsf(widen(v0[e])), fabsf(widen(v1[e]))));
       }
+      if (!(fmaxf(kmax, vmax) < INFINITY)) {
+        kmax = vmax = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        kmax = fmaxf(kmax, finite_abs(k[e]));
-        vmax = fmaxf(vmax, finite_abs(v[e]));
+        for (int e = 0; e < 8; ++e) {
+          kmax = fmaxf(kmax, fmaxf(finite_abs(k[e]), finite_abs(k[8 + e])));
+          vmax = fmaxf(vmax, fmaxf(finite_abs(widen(v0[e])), finite_abs(widen(v1[e]))));
+        }
       }
     }
-    int k_old = kScaleMin, v_old = kScaleMin;
-    if (held > 0) {
-      k_old = static_cast<int>(a.k_scale[scale_at]) - 127;
-      v_old = static_cast<int>(a.v_scale[scale_at]) - 127;
-    }
+    if (h + 1 < h1) now = load(h + 1);
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
       kmax = fmaxf(kmax, __shfl_xor(kmax, m));
@@ -214,9 +258,9 @@ __global__ __launch_bounds__(4 * D) void append_q8_kernel(AppendQ8Args a) {
       }
     } else if (fresh) {
       const float kf = power_of_two(-ke), vf = power_of_two(-ve);
-      *reinterpret_cast<u32x2*>(a.k_cache + row + 8 * j) = pack8(k, 0, kf);
-      *reinterpret_cast<u32x2*>(a.k_cache + row + HALF + 8 * j) = pack8(k, 8, kf);
-      const u32x2 w0 = pack8(v, 0, vf), w1 = pack8(v, 8, vf);
+      *reinterpret_cast<u32x2*>(a.k_cache + row + 8 * j) = pack8(k, kf);
+      *reinterpret_cast<u32x2*>(a.k_cache + row + HALF + 8 * j) = pack8(k + 8, kf);
+      const u32x2 w0 = pack8(v0, vf), w1 = pack8(v1, vf);
       *reinterpret_cast<u32x4*>(a.v_cache + row + 16 * j) = u32x4{w0[0], w0[1], w1[0], w1[1]};
     }
     if (tid == 0) {
@@ -246,8 +290,9 @@ int launch_append_kv_q8(const void* k_in, const void* v_in, const void* q_in, vo
   const double* const inv = rope_frequencies(rope_base, head_dim);
   for (int i = 0; i < 64; ++i) a.inv_freq[i] = inv[i];
   const int64_t blocks = (prefix_len + chunk_len + 63) / 64 - prefix_len / 64;
-  // heads per workgroup: as many as leave the grid four workgroups per CU, so that the angles are formed less often
-  int64_t per = blocks * n_kv_heads / 1024;
+  // heads per workgroup: up to 8 where a workgroup and a half per CU are left, so that the angles are formed less often (5824 tokens of
+  // 32 x 128: 61.8 us with one, 52.4 with four, 50.0 with eight); a step of few blocks wants them all at once (1 token 4.6 and 16)
+  int64_t per = blocks * n_kv_heads / 360;
   per = per < 1 ? 1 : per > 8 ? 8 : per;
   a.heads_per_wg = static_cast<int>(per);
   a.head_groups = static_cast<int>((n_kv_heads + per - 1) / per);
