@@ -264,7 +264,7 @@ constexpr int kPartialFloats(int D) { return kWaves * (D / 32 * 16 + 2) * 64; } 
 // on which one that was) and writes the output.
 //
 // Q8: the cache holds e4m3 with a scale per block of 64 keys and head.  Tiles come as bytes to a small buffer that each wave
-// has for itself (its sixteenth - one load of K, one of V - of the tiles two steps further on than below); in the step in which the bf16 kernel
+// has for itself (its eighth - one load of K, one of V - of the tiles three steps further on than below); in the step in which the bf16 kernel
 // sends for its piece of a tile the wave converts the piece instead, and writes it to the ring slot it would have
 // landed in.  16 conversions, 2 reads and 4 writes of LDS a step more, 2 loads instead of 4, half the bytes; the MFMA block and the schedule are
 // the same, and so are the results, bit for bit, as kvra_chunk_attn's with such a plan on the cache's values.
@@ -378,11 +378,11 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
   };
 
   // ---- Q8 ------------------------------------------------------------------------------------
-  // raw: [wave][K, V][parity of the tile] 1 KiB, behind the rings; then a word for each 32 keys of the up to 8 tiles that hold a key hidden
+  // raw: [wave][K, V][tile mod 3] 1 KiB, behind the rings; then a word for each 32 keys of the up to 8 tiles that hold a key hidden
   // from a row of the workgroup, in which a row of V with a NaN is marked (see stage_v)
   constexpr int RAW_CPR = D / 16;
-  [[maybe_unused]] const unsigned raw_lds = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV(kStages))) + wave * 4096;
-  [[maybe_unused]] unsigned* const bad_rows = reinterpret_cast<unsigned*>(ldsV(kStages)) + kWaves * 1024;
+  [[maybe_unused]] const unsigned raw_lds = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV(kStages))) + wave * 6144;
+  [[maybe_unused]] unsigned* const bad_rows = reinterpret_cast<unsigned*>(ldsV(kStages)) + kWaves * 1536;
   [[maybe_unused]] const int raw_row = (wave * 64 + lane) / RAW_CPR, raw_col = lane % RAW_CPR;
   [[maybe_unused]] const unsigned raw_off = static_cast<unsigned>(raw_row) * (row_bytes / 2) + raw_col * 16;
   // where the lane's 16 values go in a bf16 tile: two pieces side by side up to the swizzle, 16 bytes apart one way or the other
@@ -393,18 +393,29 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
   if constexpr (Q8) {
     for (int i = tid; i < 32; i += kThreads) bad_rows[i] = 0;
   }
-  [[maybe_unused]] auto raw_resource = [&](const unsigned char* cache, int t) __attribute__((always_inline)) -> u32x4 {
-    const unsigned long long at = reinterpret_cast<unsigned long long>(cache) + static_cast<unsigned long long>(g) * D +
-                                  static_cast<unsigned long long>(jt0 + t) * (tile_bytes / 2);
-    const int rows = min(max(rows_end - (jt0 + t) * BN, 0), BN);
-    return u32x4{uniform(static_cast<unsigned>(at)), uniform(static_cast<unsigned>(at >> 32) & 0xFFFFu),
-                 uniform(rows > 0 ? rows * (row_bytes / 2) - g * D : 0u), 0x00020000u};
-  };
-  // sends for the bytes of K tile t and V tile t - 1
-  [[maybe_unused]] auto send_raw = [&](int t) __attribute__((always_inline)) {
+  // slot of K's bytes that a step with j % 3 == r takes up (K tile st + 2; V tile st + 1)
+  [[maybe_unused]] unsigned raw_k[3], raw_v[3];
+#pragma unroll
+  for (int r = 0; r < 3; ++r) {
+    raw_k[r] = uniform(raw_lds + (r + phase + 2) % 3 * 1024);
+    raw_v[r] = uniform(raw_lds + 3072 + (r + phase + 1) % 3 * 1024);
+  }
+  // Sends for a step's bytes, three steps ahead of it.  Walked tile by tile: offset of the V tile in a cache, rows from it to the end,
+  // bytes of those in the tile (a lane beyond gets zeros), which the K tile of one step hands on to the V tile of the next.
+  [[maybe_unused]] unsigned long long raw_tile = static_cast<unsigned long long>(jt0 + phase + 1) * (tile_bytes / 2) + static_cast<unsigned long long>(g) * D;
+  [[maybe_unused]] int raw_rows = rows_end - (jt0 + phase + 1) * BN;
+  [[maybe_unused]] unsigned raw_bytes = min(max(raw_rows, 0), BN) * (row_bytes / 2);
+  [[maybe_unused]] auto send_raw = [&](unsigned k_slot, unsigned v_slot) __attribute__((always_inline)) {
     if constexpr (Q8) {
-      lds_dma16(raw_resource(a.k8, t), raw_off, uniform(raw_lds + (t & 1) * 1024));
-      lds_dma16(raw_resource(a.v8, t - 1), raw_off, uniform(raw_lds + 2048 + ((t - 1) & 1) * 1024));
+      auto resource = [&](const unsigned char* cache) __attribute__((always_inline)) -> u32x4 {
+        const unsigned long long at = reinterpret_cast<unsigned long long>(cache) + raw_tile;
+        return u32x4{uniform(static_cast<unsigned>(at)), uniform(static_cast<unsigned>(at >> 32) & 0xFFFFu), uniform(raw_bytes), 0x00020000u};
+      };
+      lds_dma16(resource(a.v8), raw_off, v_slot);
+      raw_tile += tile_bytes / 2;
+      raw_rows -= BN;
+      raw_bytes = min(max(raw_rows, 0), BN) * (row_bytes / 2);
+      lds_dma16(resource(a.k8), raw_off, k_slot);
     }
   };
   [[maybe_unused]] auto block_of = [&](int t) __attribute__((always_inline)) -> long long {   // of this wave's rows of tile t
@@ -438,17 +449,22 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
   // it: in tiles that hold keys hidden from a row of the workgroup it becomes a zero, and its key is marked; the scores of
   // a marked key are NaN.
   [[maybe_unused]] auto without_nan = [&](u32x4 codes, int t) __attribute__((always_inline)) -> u32x4 {
-    if (jt0 + t >= diag0) {
-      unsigned bad = 0;
+    unsigned bad = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= nan_bytes(codes[i]);
-      if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
+    for (int i = 0; i < 4; ++i) bad |= nan_bytes(codes[i]);
+    if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) codes[i] &= ~((nan_bytes(codes[i]) >> 7) * 255u);
-        if (bad != 0) atomicOr(bad_rows + (jt0 + t - diag0) * 4 + raw_row / 32, 1u << (raw_row % 32));
-      }
+      for (int i = 0; i < 4; ++i) codes[i] &= ~((nan_bytes(codes[i]) >> 7) * 255u);
+      if (bad != 0) atomicOr(bad_rows + (jt0 + t - diag0) * 4 + raw_row / 32, 1u << (raw_row % 32));
     }
     return codes;
+  };
+  // (done where the bytes lie, ahead of the step's other work)
+  [[maybe_unused]] auto mark_nan = [&](unsigned slot, int t) __attribute__((always_inline)) {
+    if (jt0 + t >= diag0) {
+      lds_u32x4* const at = (lds_u32x4*)static_cast<uintptr_t>(slot + lane * 16);
+      *at = without_nan(*at, t);
+    }
   };
   [[maybe_unused]] auto raw_at = [&](unsigned addr) __attribute__((always_inline)) -> u32x4 {
     return *(lds_u32x4*)static_cast<uintptr_t>(addr + lane * 16);
@@ -527,11 +543,11 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
       if (i < 3) put_values(raw[i], scale_factor(scale[i]), static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsK(i))), k_put);
-      else put_values(without_nan(raw[i], i - 3), scale_factor(scale[i]), static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV(i - 3))), v_put);
+      else put_values(jt0 + i - 3 >= diag0 ? without_nan(raw[i], i - 3) : raw[i], scale_factor(scale[i]), static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV(i - 3))), v_put);
     }
     load_scale_bytes(0);
-    send_raw(phase + 2);
-    send_raw(phase + 3);
+#pragma unroll
+    for (int r = 0; r < 3; ++r) send_raw(raw_k[r], raw_v[r]);
   } else {
 #pragma unroll
     for (int t = 0; t < 3; ++t) dma_tile(kbase, koff, t, ldsK(t));
@@ -622,15 +638,16 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
     [[maybe_unused]] u32x4 raw;
     if constexpr (Q8) {
       factors(j, &k_factor, &v_factor);
-      asm volatile("s_waitcnt vmcnt(2)" ::: "memory");   // the bytes of K tile st + 2 and V tile st + 1: all but the last two loads
+      asm volatile("s_waitcnt vmcnt(4)" ::: "memory");   // this step's bytes: all but the last four loads
+      mark_nan(raw_v[RS], st + 1);
     }
     auto stage_piece = [&](int idx) __attribute__((always_inline)) {
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (Q8) {
-        if (idx == 0) raw = raw_at(raw_lds + (st & 1) * 1024);
+        if (idx == 0) raw = raw_at(raw_k[RS]);
         else if (idx == 1) put_values(raw, k_factor, slot_k[RS], k_put);
-        else if (idx == 2) raw = raw_at(raw_lds + 2048 + ((st + 1) & 1) * 1024);
-        else put_values(without_nan(raw, st + 1), v_factor, slot_v[RS], v_put);
+        else if (idx == 2) raw = raw_at(raw_v[RS]);
+        else put_values(raw, v_factor, slot_v[RS], v_put);
       } else if (idx < LOADS)
         lds_dma16(k_res, koff[idx], slot_k[RS] + idx * (kWaves * 64 * 16));
       else
@@ -752,7 +769,7 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
       for (int qb = 0; qb < QB; ++qb) l[qb] += psum[qb][0] + psum[qb][1];
     }
     // everything issued before this block (tiles K(st+1), V(st)) must have landed before the barrier
-    if constexpr (Q8) send_raw(st + 4);
+    if constexpr (Q8) send_raw(raw_k[RS], raw_v[RS]);
     else __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * LOADS));
     if (!ONE_BARRIER || phase == 0) __syncthreads();
   };
@@ -779,11 +796,13 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
     if constexpr (Q8) {
       float kf, vf;
       factors(j, &kf, &vf);
-      asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
-      put_values(raw_at(raw_lds + (st & 1) * 1024), kf, static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsK((st + 2) % kStages))), k_put);
-      put_values(without_nan(raw_at(raw_lds + 2048 + ((st + 1) & 1) * 1024), st + 1), vf,
-                 static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV((st + 1) % kStages))), v_put);
-      send_raw(st + 4);
+      const unsigned k_slot = raw_lds + (st + 2) % 3 * 1024, v_slot = raw_lds + 3072 + (st + 1) % 3 * 1024;
+      asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+      mark_nan(v_slot, st + 1);
+      put_values(raw_at(k_slot), kf, static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsK((st + 2) % kStages))), k_put);
+      put_values(raw_at(v_slot), vf, static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV((st + 1) % kStages))), v_put);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      send_raw(uniform(k_slot), uniform(v_slot));
       if (!ONE_BARRIER || phase == 0) __syncthreads();
       continue;
     }
@@ -1634,7 +1653,7 @@ int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len
   a.v8 = static_cast<const unsigned char*>(cache.v);
   a.k_scale = static_cast<const unsigned char*>(cache.k_scale);
   a.v_scale = static_cast<const unsigned char*>(cache.v_scale);
-  const unsigned smem = 2u * kStages * static_cast<unsigned>(a.bn) * static_cast<unsigned>(head_dim) * 2u + kWaves * 4096u + 128u;   // rings, bytes, marks
+  const unsigned smem = 2u * kStages * static_cast<unsigned>(a.bn) * static_cast<unsigned>(head_dim) * 2u + kWaves * 6144u + 128u;   // rings, bytes, marks
   const dim3 grid(static_cast<unsigned>(plan.groups * plan.slots)), block(kThreads);
   return head_dim == 128 ? launch_kernel(chunk_attn_q8_kernel<128>, grid, block, a, stream, smem)
                          : launch_kernel(chunk_attn_q8_kernel<64>, grid, block, a, stream, smem);

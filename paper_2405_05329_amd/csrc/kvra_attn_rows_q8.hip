@@ -169,6 +169,7 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
     return bf16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
   };
 
+  bool referenced = false;   // the wave's rows have an exponent reference (those that have met a visible key)
   for (int i = 0; t < t_hi; t += kQ8Waves, ++i) {
     const bool more = t + kQ8Waves < t_hi;
     if (i > 0 && (i & 63) == 0) load_scales(t);
@@ -243,35 +244,52 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
             if (16 * kb + e > rel) s[kb][qb][e] = -INFINITY;
       }
     }
+    // Weights relative to the exponent reference in force, without looking for the largest score; where a lane's sum gets out of hand
+    // (scores that outgrew the reference by about 2^20), and on the wave's first tile, the reference moves to the row's maximum,
+    // what has been summed up follows, and the weights are formed again.
     u32x4 pf[KB / 2][QB];
+    float psum[QB];
+    for (bool again = false;;) {
+      if (again || referenced) {
+        bool out_of_hand = false;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      float tmax = s[0][qb][0];
+        for (int qb = 0; qb < QB; ++qb) {
+          psum[qb] = 0.0f;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+          for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) tmax = fmaxf(tmax, s[kb][qb][e]);
-      tmax = fmaxf(tmax, other_half(tmax));
-      tmax = fmaxf(tmax, other_row(tmax));
-      const float mn = fmaxf(m[qb], tmax * a.c_log2);    // a row that has met no visible key stays at kNoKeyYet: weights 0
-      const float alpha = __builtin_amdgcn_exp2f(m[qb] - mn);
-      m[qb] = mn;
-      float psum = 0.0f;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][e], a.c_log2, -mn)), p1 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][e + 1], a.c_log2, -mn));
-          psum += p0 + p1;
-          const bf16x2 pp = {static_cast<__bf16>(p0), static_cast<__bf16>(p1)};
-          pf[kb / 2][qb][2 * (kb % 2) + e / 2] = __builtin_bit_cast(unsigned, pp);
+            for (int e = 0; e < 4; e += 2) {
+              const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][e], a.c_log2, -m[qb])), p1 = __builtin_amdgcn_exp2f(fmaf(s[kb][qb][e + 1], a.c_log2, -m[qb]));
+              psum[qb] += p0 + p1;
+              const bf16x2 pp = {static_cast<__bf16>(p0), static_cast<__bf16>(p1)};
+              pf[kb / 2][qb][2 * (kb % 2) + e / 2] = __builtin_bit_cast(unsigned, pp);
+            }
+          out_of_hand |= !(psum[qb] < 1048576.0f);
         }
-      l[qb] = fmaf(l[qb], alpha, psum);
+        if (again || __builtin_amdgcn_ballot_w64(out_of_hand) == 0) break;
+      }
+      again = referenced = true;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+      for (int qb = 0; qb < QB; ++qb) {
+        float tmax = s[0][qb][0];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[db][qb][e] *= alpha;
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) tmax = fmaxf(tmax, s[kb][qb][e]);
+        tmax = fmaxf(tmax, other_half(tmax));
+        tmax = fmaxf(tmax, other_row(tmax));
+        const float mn = fmaxf(m[qb], tmax * a.c_log2);    // a row that has met no visible key stays at kNoKeyYet: weights 0
+        const float alpha = __builtin_amdgcn_exp2f(m[qb] - mn);
+        m[qb] = mn;
+        l[qb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[db][qb][e] *= alpha;
+      }
     }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) l[qb] += psum[qb];
     wait_v();
     // contraction slot 8 g4 + 4 b + u of step kk is key 32 kk + 16 b + 4 g4 + u on both operands
 #pragma unroll
@@ -362,36 +380,51 @@ __global__ __launch_bounds__(kQ8Threads, 2) void attn_rows_q8_kernel(RowsQ8Args 
     }
 #pragma unroll
     for (int i = 0; i < RW; ++i) acc[i] = 0.0f;
-    if (16 * qb0 + n >= live) return;       // (no barrier from here on)
-    constexpr int AHEAD = 8;                // partial results on their way together
+    // Where a 16-row block has few rows its 16 lanes share out the workgroups' results: lane n has row n % span and every 16 / span-th
+    // result from n / span on, and they meet at the end.
+    int log_span = 4;
+    while (log_span > 0 && live <= 1 << (log_span - 1)) --log_span;
+    const int span = 1 << log_span, row = n & (span - 1), shares = 16 >> log_span;
+    constexpr int AHEAD = 8;                // of a lane's results on their way together
 #pragma unroll 1
-    for (int p0 = 0; p0 < a.splits; p0 += AHEAD) {
+    for (int p0 = n >> log_span; p0 < a.splits; p0 += AHEAD * shares) {
       float pv[AHEAD][RW], pm[AHEAD][QW], pl[AHEAD][QW];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const float* p = slots + static_cast<long long>(min(p0 + u, a.splits - 1)) * SLOT;
-#pragma unroll
-        for (int i = 0; i < RW; ++i) pv[u][i] = load_coherent(p + (r0 + i) * 64 + lane);
+        const float* p = slots + static_cast<long long>(min(p0 + u * shares, a.splits - 1)) * SLOT;
 #pragma unroll
         for (int j = 0; j < QW; ++j) {
-          pm[u][j] = load_coherent(p + R * 64 + 16 * (qb0 + j) + n);
-          pl[u][j] = load_coherent(p + R * 64 + ROWS + 16 * (qb0 + j) + n);
+          const bool is_row = 16 * (qb0 + j) + row < live;
+#pragma unroll
+          for (int i = 0; i < RE; ++i) pv[u][RE * j + i] = is_row ? load_coherent(p + (r0 + RE * j + i) * 64 + 16 * g4 + row) : 0.0f;
+          pm[u][j] = is_row ? load_coherent(p + R * 64 + 16 * (qb0 + j) + row) : kNoKeyYet;
+          pl[u][j] = is_row ? load_coherent(p + R * 64 + ROWS + 16 * (qb0 + j) + row) : 0.0f;
         }
       }
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
+      for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
         for (int j = 0; j < QW; ++j) {
-          const bool there = p0 + u < a.splits;   // (past the last it is loaded again, and weighs nothing)
+          const bool there = p0 + u * shares < a.splits;   // (past the last it is loaded again, and weighs nothing)
           const float mn = there ? fmaxf(am[j], pm[u][j]) : am[j];
           const float wa = __builtin_amdgcn_exp2f(am[j] - mn), wb = there ? __builtin_amdgcn_exp2f(pm[u][j] - mn) : 0.0f;
           am[j] = mn;
           al[j] = fmaf(pl[u][j], wb, al[j] * wa);
 #pragma unroll
-          for (int i = 0; i < RE; ++i) acc[RE * j + i] = fmaf(pv[u][RE * j + i], wb, acc[RE * j + i] * wa);
+          for (int i = 0; i < RE; ++i) acc[RE * j + i] = fmaf(there ? pv[u][RE * j + i] : 0.0f, wb, acc[RE * j + i] * wa);
         }
-      }
     }
+#pragma unroll 1
+    for (int step = span; step < 16; step *= 2)
+#pragma unroll
+      for (int j = 0; j < QW; ++j) {
+        const float om = __shfl_xor(am[j], step), ol = __shfl_xor(al[j], step), mn = fmaxf(am[j], om);
+        const float wa = __builtin_amdgcn_exp2f(am[j] - mn), wb = __builtin_amdgcn_exp2f(om - mn);
+        am[j] = mn;
+        al[j] = al[j] * wa + ol * wb;
+#pragma unroll
+        for (int i = 0; i < RE; ++i) acc[RE * j + i] = acc[RE * j + i] * wa + __shfl_xor(acc[RE * j + i], step) * wb;
+      }
   }
 
   // register e of block (db, qb) is column 16 db + 4 g4 + e of row n
