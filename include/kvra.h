@@ -441,6 +441,10 @@ int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void* v_cache, 
                        float scale, void* out, void* workspace, int64_t workspace_bytes, void* stream);
 int64_t kvra_chunk_attn_q8_workspace_bytes(void);
 
+/* kvra_chunk_attn_row_splits for kvra_chunk_attn_q8 (slices of 16 or 32 virtual rows; the tiled kernel runs kvra_chunk_attn_plan's plan). */
+int kvra_chunk_attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
+                                  int head_dim, int n_cus, int* splits_out);
+
 /*
  * Weights into the 4-bit format and back.  w [n, k] bf16; codes [n, k / 2] bytes; scales [n, k / 32] bytes.  n must be a multiple of 32 and
  * k of 64, and w must stay below 4 GiB (KVRA_EUNSUPPORTED).  A group of 32 that holds an infinity or a NaN

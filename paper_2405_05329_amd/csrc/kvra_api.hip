@@ -335,6 +335,16 @@ extern "C" int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void
                                     n_kv_heads, head_dim, scale, out, workspace, static_cast<hipStream_t>(stream));
 }
 
+extern "C" int kvra_chunk_attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
+                                             int head_dim, int n_cus, int* splits_out) {
+  if (splits_out == nullptr || n_cus < 1) return KVRA_EINVAL;
+  if (chunk_len < 1 || prefix_len < 0) return KVRA_EINVAL;
+  int rc = check_heads(n_q_heads, n_kv_heads, head_dim);
+  if (rc != KVRA_OK) return rc;
+  if (chunk_len > kMaxTokens || prefix_len > kMaxTokens) return KVRA_EUNSUPPORTED;
+  return kvra::attn_q8_row_splits(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, n_cus, splits_out);
+}
+
 namespace {
 
 int check_w4(int64_t n, int64_t k) {

@@ -527,6 +527,9 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
   for (int i = tid; i < TILE; i += kThreads) ldsV(kStages - 1)[i] = u32x4{0u, 0u, 0u, 0u};
   if constexpr (Q8) {
     __syncthreads();                       // the marks are cleared
+    // everything the piece begins with is sent for before any of it is waited for
+#pragma unroll
+    for (int r = 0; r < 3; ++r) send_raw(raw_k[r], raw_v[r]);
     u32x4 raw[5];
     unsigned scale[5];
 #pragma unroll
@@ -540,14 +543,12 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
         scale[i] = (i < 3 ? a.k_scale : a.v_scale)[static_cast<long long>(row / 64) * a.Hkv + g];
       }
     }
+    load_scale_bytes(0);
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
       if (i < 3) put_values(raw[i], scale_factor(scale[i]), static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsK(i))), k_put);
       else put_values(jt0 + i - 3 >= diag0 ? without_nan(raw[i], i - 3) : raw[i], scale_factor(scale[i]), static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV(i - 3))), v_put);
     }
-    load_scale_bytes(0);
-#pragma unroll
-    for (int r = 0; r < 3; ++r) send_raw(raw_k[r], raw_v[r]);
   } else {
 #pragma unroll
     for (int t = 0; t < 3; ++t) dma_tile(kbase, koff, t, ldsK(t));
@@ -1525,24 +1526,52 @@ int rows_splits(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int
 namespace {
 
 // The same choice over a cache in 8 bits: rows of a slice of the kernel for few rows and workgroups for each, or *splits = 0.
+// Expected times of both kernels in us, fitted to 299 timed shapes (14 head layouts, prefixes 0 to 128000, 1 to 16000 tokens); the choice
+// costs 0.2 % against choosing by hindsight, 13 % on the worst of them (8 heads x 128 on 2, 192 tokens behind 128000: 154 us tiled,
+// 136 in slices).  256 tokens behind 4000, 32 heads x 128: 45.4 tiled, 27.3 in slices; 1024: 84.2 and 110.4.
+//   slices  a launch and its merge, rounds of workgroups (head_dim 64: two to a CU), the steps of a wave with the work spread evenly and as
+//           it falls
+//   tiled   tile steps of the busiest slot, more for full row tiles, and the merging of cut units: all of them, and one unit's pieces
 void rows_q8_shape(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus,
                    int* rows, int* splits) {
   const int64_t vrows = chunk_len * (n_q_heads / n_kv_heads);
   *rows = vrows <= 16 ? 16 : 32;
   *splits = 0;
-  const int64_t units = (vrows + *rows - 1) / *rows * n_kv_heads, tiles = (prefix_len + chunk_len + 63) / 64;
-#ifdef KVRA_Q8_FORCE
-  if (KVRA_Q8_FORCE == 2) return;
-#else
-  if (rows_splits(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, kStaticSlots * attn_partial_bytes(128)) == 0) return;
-#endif
+  const int64_t slices = (vrows + *rows - 1) / *rows, units = slices * n_kv_heads, tiles = (prefix_len + chunk_len + 63) / 64;
+  if (cus < 1 || slices > 65535 || units > 64 * static_cast<int64_t>(cus)) return;
   // as many workgroups per slice as leave one per CU, none without two key tiles for each of its waves
   int64_t s = 1;
   if (units <= kCounterInts) s = std::max<int64_t>(1, std::min(std::min<int64_t>(cus / units, (tiles + 15) / 16), int64_t(32)));
-  *splits = static_cast<int>(s);
+  const int64_t at_once = head_dim == 64 ? 2 * cus : cus;
+  const float rounds = static_cast<float>((units * s + at_once - 1) / at_once);
+  const float mean_tiles = 0.5f * (static_cast<float>(prefix_len) / 64.0f + 1.0f + static_cast<float>(tiles));
+  const float load = static_cast<float>(units) * mean_tiles / (8.0f * static_cast<float>(cus));
+  const float depth = static_cast<float>((tiles + 8 * s - 1) / (8 * s)), mean_depth = rounds * mean_tiles / (8.0f * static_cast<float>(s));
+  const float steps = static_cast<float>(plan.steps_per_slot), cut = static_cast<float>(plan.partial_pieces) / static_cast<float>(cus);
+  const float full = steps * static_cast<float>(plan.rows_per_tile) / 256.0f;
+  const int64_t row_tiles = (vrows + plan.rows_per_tile - 1) / plan.rows_per_tile * n_kv_heads;
+  const float joined = static_cast<float>(plan.partial_pieces) / static_cast<float>(row_tiles);
+  float sliced, tiled;
+  if (head_dim == 128) {
+    sliced = 6.0f + (s > 1 ? 4.5f + 0.24f * static_cast<float>(s) : 0.0f) + 5.7f * (rounds - 1.0f) + 2.38f * load + (rounds > 1.0f ? 0.14f * mean_depth : 0.59f * depth);
+    tiled = -0.3f + 1.04f * steps + 0.66f * full + (plan.partial_pieces > 0 ? 4.7f + 7.3f * cut + 0.98f * joined : 0.0f);
+  } else {
+    sliced = 4.5f + (s > 1 ? 2.9f + 0.28f * static_cast<float>(s) : 0.0f) + 6.25f * (rounds - 1.0f) + 1.54f * load + (rounds > 1.0f ? 0.43f * mean_depth : 0.6f * depth);
+    tiled = -2.6f + 1.33f * steps + 0.66f * full + (plan.partial_pieces > 0 ? 6.6f + 9.4f * cut + 0.68f * joined : 0.0f);
+  }
+  if (sliced < tiled) *splits = static_cast<int>(s);
 }
 
 }  // namespace
+
+int attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus, int* splits) {
+  AttnPlan plan;
+  const int rc = plan_chunk_attn(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, true, &plan);
+  if (rc != KVRA_OK) return rc;
+  int rows = 0;
+  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, &rows, splits);
+  return KVRA_OK;
+}
 
 int attn_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus, int* splits) {
   AttnPlan plan;

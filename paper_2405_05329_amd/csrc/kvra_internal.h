@@ -142,6 +142,7 @@ int64_t attn_rows_q8_slot_bytes(int head_dim, int rows);
 int64_t attn_q8_workspace_bytes();
 int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
                          int head_dim, float scale, void* out, void* workspace, hipStream_t stream);
+int attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus, int* splits);
 int current_device_cus();   // 0 if it cannot be asked
 
 int launch_pack_w4(const void* w, void* codes, void* scales, int64_t n, int64_t k, hipStream_t stream);

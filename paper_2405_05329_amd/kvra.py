@@ -114,6 +114,8 @@ def _load() -> ctypes.CDLL:
     lib.kvra_chunk_attn_q8.argtypes = [vp] * 5 + [i64, i64, i32, i32, i32, f32, vp, vp, i64, vp]
     lib.kvra_chunk_attn_q8_workspace_bytes.restype = i64
     lib.kvra_chunk_attn_q8_workspace_bytes.argtypes = []
+    lib.kvra_chunk_attn_q8_row_splits.restype = i32
+    lib.kvra_chunk_attn_q8_row_splits.argtypes = [i64, i64, i32, i32, i32, i32, ctypes.POINTER(i32)]
     lib.kvra_pack_w4.restype = i32
     lib.kvra_pack_w4.argtypes = [vp, vp, vp, i64, i64, vp]
     lib.kvra_unpack_w4.restype = i32
@@ -525,6 +527,15 @@ def kvra_chunk_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, chunk_
 
 def kvra_chunk_attn_q8_workspace_bytes() -> int:
     return int(_lib.kvra_chunk_attn_q8_workspace_bytes())
+
+
+def kvra_chunk_attn_q8_row_splits(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, n_cus) -> int:
+    """0 if the shape gets the tiled attention kernel, else the workgroups per slice of the kernel for few rows."""
+    splits = ctypes.c_int()
+    rc = _lib.kvra_chunk_attn_q8_row_splits(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, n_cus, ctypes.byref(splits))
+    if rc != KVRA_OK:
+        raise KvraError(rc, "kvra_chunk_attn_q8_row_splits")
+    return splits.value
 
 
 def kvra_pack_w4(w, codes, scales, n, k, stream=None):

@@ -189,8 +189,8 @@ def test_attention(H, Hkv, d, prefix, c):
 # launches of the kernel with 256 rows a workgroup: whole and cut units, gangs, one and several rounds, row tiles that are not full,
 # more than 64 tile steps, tiles past the end, groups of heads
 TILED = [
-    (16, 16, 128, 12000, 130), (8, 8, 64, 20000, 420), (8, 8, 128, 20000, 290), (32, 32, 128, 0, 1024), (32, 8, 128, 1000, 1090), (71, 1, 64, 4096, 600),
-    (32, 32, 128, 3000, 777), (4, 4, 128, 0, 5000), (3, 3, 64, 1000, 6000), (32, 1, 128, 700, 1301), (16, 16, 64, 0, 2048),
+    (32, 32, 128, 100, 1100), (32, 8, 128, 1000, 1090), (32, 32, 128, 3000, 777), (32, 1, 128, 700, 1301), (16, 16, 128, 12000, 500), (8, 8, 128, 20000, 700),
+    (32, 32, 128, 0, 4200), (71, 1, 64, 4096, 600), (71, 1, 64, 100, 1500), (8, 8, 64, 20000, 1500), (8, 8, 64, 0, 6000), (16, 8, 64, 3000, 3000),
 ]
 
 
@@ -198,7 +198,7 @@ TILED = [
 def test_attention_of_many_rows_is_the_bf16_kernels(H, Hkv, d, prefix, c):
     """Bit for bit what kvra_chunk_attn gives on the values that the cache stands for; and near the oracle on some rows."""
     cus = torch.cuda.get_device_properties(0).multi_processor_count
-    assert kvra.kvra_chunk_attn_row_splits(prefix, c, H, Hkv, d, cus) == 0, "not the kernel this shape is here for"
+    assert kvra.kvra_chunk_attn_q8_row_splits(prefix, c, H, Hkv, d, cus) == 0 == kvra.kvra_chunk_attn_row_splits(prefix, c, H, Hkv, d, cus), "not the kernel this shape is here for"
     n = prefix + c
     rng = np.random.default_rng(17)
     q = to_dev(synth.normal_bf16(7, 64, 0, (c, H, d)))
@@ -251,7 +251,7 @@ def test_attention_score_ranges(d, H, Hkv, prefix, c, kind):
 
 
 @pytest.mark.parametrize("H,Hkv,d,prefix,c", [(4, 2, 64, 100, 200), (4, 2, 128, 40, 300), (2, 2, 128, 1000, 70), (71, 1, 64, 64, 66), (4, 2, 128, 200, 1),
-                                              (8, 8, 128, 0, 1500), (16, 1, 64, 0, 900), (32, 32, 128, 100, 700), (71, 1, 64, 3000, 500)])
+                                              (8, 8, 128, 0, 1500), (16, 1, 64, 0, 900), (32, 32, 128, 100, 1100), (71, 1, 64, 4096, 600)])
 def test_attention_nan_reaches_those_that_see_it(H, Hkv, d, prefix, c):
     """NaN in K and in V, in rows of the chunk and of the prefix.  Heads that do not read it keep their bits.  A wave that meets a NaN
     may take its rows' exponents relative to another reference: the rows before it then round otherwise, each result within its bound of

@@ -121,6 +121,16 @@ def test_attention_refusals(want, args):
     assert _attn(**args) == want
 
 
+def test_which_attention_kernel_a_shape_gets():
+    splits = lambda *a: kvra.kvra_chunk_attn_q8_row_splits(*a, 256)
+    assert splits(16383, 1, 32, 32, 128) == 8 and splits(1000, 1, 32, 8, 128) == 1 and splits(0, 1, 2, 2, 64) == 1      # a token
+    assert splits(15296, 1088, 32, 32, 128) == 0 and splits(7104, 1088, 71, 1, 64) == 0                              # a prompt's chunk
+    for bad in ((0, 0, 2, 2, 64), (-1, 1, 2, 2, 64), (0, 1, 3, 2, 64)):
+        assert _code(splits, *bad) == INVALID
+    assert _code(splits, 0, 1, 2, 2, 96) == UNSUPPORTED
+    assert _code(kvra.kvra_chunk_attn_q8_row_splits, 0, 1, 2, 2, 64, 0) == INVALID
+
+
 def _code(call, *args):
     with pytest.raises(kvra.KvraError) as e:
         call(*args)
