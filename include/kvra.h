@@ -414,7 +414,8 @@ int kvra_layer_chunk(const kvra_layer* layer, const void* x, void* y, void* k_ca
  * exception: where the chunk starts inside a block, the scale found there (that of an earlier append; rows
  * of the block ahead of prefix_len are taken to be valid) never shrinks, and if a new value asks for a larger one, the
  * block's earlier rows are rescaled, which is exact for all but values below the smallest normal number of
- * the new scale.  A cache needs no initialisation.
+ * the new scale.  A cache needs no initialisation.  Calls that work on rows of one block (an append and another, or an
+ * append and attention over what lies ahead of it) have to be ordered, by a stream or by events.
  * A NaN or an infinity is stored as NaN and does not count towards the scale.
  * Errors: KVRA_EINVAL, KVRA_EUNSUPPORTED, KVRA_ERANGE, KVRA_ELAUNCH, as kvra_append_kv.
  */

@@ -1538,7 +1538,7 @@ void rows_q8_shape(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, 
   *rows = vrows <= 16 ? 16 : 32;
   *splits = 0;
   const int64_t slices = (vrows + *rows - 1) / *rows, units = slices * n_kv_heads, tiles = (prefix_len + chunk_len + 63) / 64;
-  if (cus < 1 || slices > 65535 || units > 64 * static_cast<int64_t>(cus)) return;
+  if (cus < 1 || slices > 65535) return;   // (a grid's third dimension)
   // as many workgroups per slice as leave one per CU, none without two key tiles for each of its waves
   int64_t s = 1;
   if (units <= kCounterInts) s = std::max<int64_t>(1, std::min(std::min<int64_t>(cus / units, (tiles + 15) / 16), int64_t(32)));

@@ -138,8 +138,10 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
   struct Chunk {
     u32x4 w[RB], x[XL];
   };
-  // (Chunks behind the wave's share are loaded and left.)
+  // (A chunk behind the wave's share is loaded and left; one behind the rows' end is the last again: a scalar offset has to stay inside
+  // the resource, the lanes' offsets are compared with what is left of it.)
   auto load = [&](Chunk& b, int c) __attribute__((always_inline)) {
+    c = min(c, chunks - 1);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
       b.w[rb] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(w_res[rb % MATS], static_cast<int>(w_off + rb / MATS * 16 * w_ld), 64 * c, 0));
@@ -489,12 +491,19 @@ __global__ __launch_bounds__(256 * WK, 2) void linear_w4_tile_kernel(LinearW4Arg
 namespace {
 
 template <bool DUAL, int RB, int TB, int XL, int WAVES>
-int launch_rows(LinearW4Args& a, hipStream_t stream) {
-  const int64_t tiles = (a.m + 16 * TB - 1) / (16 * TB);
-  if (tiles > 65535) return KVRA_EUNSUPPORTED;
-  return launch_kernel(linear_w4_rows_kernel<DUAL, RB, TB, XL, WAVES>,
-                       dim3(static_cast<unsigned>(a.n / (DUAL ? 8 * RB : 16 * RB)), static_cast<unsigned>(tiles)), dim3(64 * WAVES), a, stream,
-                       WAVES * (RB + 4 * TB) * 1024u);
+int launch_rows(LinearW4Args a, hipStream_t stream) {
+  constexpr int64_t MOST = 65535 * int64_t(16 * TB);     // tokens of a launch: a grid's second dimension ends there
+  for (int64_t left = a.m; left > 0; left -= MOST) {
+    a.m = static_cast<int>(std::min(left, MOST));
+    const int rc = launch_kernel(linear_w4_rows_kernel<DUAL, RB, TB, XL, WAVES>,
+                                 dim3(static_cast<unsigned>(a.n / (DUAL ? 8 * RB : 16 * RB)), static_cast<unsigned>((a.m + 16 * TB - 1) / (16 * TB))),
+                                 dim3(64 * WAVES), a, stream, WAVES * (RB + 4 * TB) * 1024u);
+    if (rc != KVRA_OK) return rc;
+    a.x += MOST * a.k;
+    a.out += MOST * a.n;
+    if (a.res != nullptr) a.res += MOST * a.n;
+  }
+  return KVRA_OK;
 }
 
 template <bool DUAL>

@@ -353,6 +353,40 @@ def test_linear(form, m, n, k):
     assert np.all(err <= bound), (float((err / bound).max()), np.argwhere(err > bound)[:3])
 
 
+def test_linear_of_more_tokens_than_a_grid_holds():
+    # 65535 tiles of 64 tokens and 70 more: the same 65 tokens over and over give the same 65 results
+    n, k, m = 32, 64, 65535 * 64 + 70
+    base = synth.normal_bf16(14, 65, 2, (65, k))
+    w, s = weights(3, n, k)
+    x = to_dev(base).repeat(m // 65 + 1, 1)[:m].contiguous()
+    r = torch.zeros(m, n, dtype=torch.bfloat16, device="cuda")
+    r[:, 0] = (torch.arange(m, device="cuda") % 128).to(torch.bfloat16)          # (residual rows of their own: exact in bf16)
+    out = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    kvra.kvra_linear_w4(x, bytes_dev(w), bytes_dev(s), None, None, None, out, m, n, k)
+    want, terms = lowbit.linear(f64(base), w, s, None, None, None)
+    bound = U * np.abs(want) * (1 + U) + (k / 32 + 48) * 2.0 ** -24 * terms + 2.0 ** -20 * np.abs(want) + 1e-30
+    assert np.all(np.abs(f64(to_bits(out[:65])) - want) <= bound)
+    assert torch.equal(out, out[:65].repeat(m // 65 + 1, 1)[:m])
+    with_residual = torch.empty_like(out)
+    kvra.kvra_linear_w4(x, bytes_dev(w), bytes_dev(s), None, None, r, with_residual, m, n, k)
+    assert torch.equal(with_residual[:, 1:], out[:, 1:])
+    col = torch.from_numpy(want[:, 0]).cuda().repeat(m // 65 + 1)[:m] + r[:, 0].double()
+    slack = 2.0 ** -8 * (1 + 2.0 ** -8) * col.abs() + 1e-5 * (1 + float(terms[:, 0].max()))     # half a step of bf16; fp32 sums of 65 terms
+    assert bool(((with_residual[:, 0].double() - col).abs() <= slack).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 32, 64), (3, 64, 1088), (17, 32, 320), (70, 512, 576)])
+def test_linear_looks_at_nothing_behind_the_last_token(m, n, k):
+    x = synth.normal_bf16(14, m, 3, (m, k))
+    w, s = weights(4, n, k)
+    behind = torch.full((m + 40, k), float("nan"), dtype=torch.bfloat16, device="cuda")
+    behind[:m] = to_dev(x)
+    a, b = torch.empty(m, n, dtype=torch.bfloat16, device="cuda"), torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    kvra.kvra_linear_w4(behind[:m], bytes_dev(w), bytes_dev(s), None, None, None, a, m, n, k)
+    kvra.kvra_linear_w4(to_dev(x), bytes_dev(w), bytes_dev(s), None, None, None, b, m, n, k)
+    assert not bool(torch.isnan(a).any()) and torch.equal(a, b)
+
+
 def test_linear_groups_of_any_magnitude_and_nan():
     """Scales from 2^-60 to 2^60 along a row; a NaN group reaches its column of the result and no other."""
     m, n, k = 3, 64, 256
