@@ -428,10 +428,12 @@ int kvra_append_kv_q8(const void* k_in, const void* v_in, const void* q_in, void
  * kvra_chunk_attn over an 8-bit cache, from one token (a step behind the prompt) to a whole chunk.
  *   q, scale, out   as kvra_chunk_attn; k_cache .. v_scale as kvra_append_kv_q8 leaves them, rows
  *               [0, prefix_len + chunk_len) valid (others are not read, whatever they hold)
- *   workspace   caller-owned device memory, 256-byte aligned, at least kvra_chunk_attn_q8_workspace_bytes() (100 MiB,
+ *   workspace   caller-owned device memory, 256-byte aligned, at least kvra_chunk_attn_q8_workspace_bytes() (128 MiB,
  *               enough for every shape).  Its first 16 KiB have to be zero before its first use, and every call leaves them
  *               zero; the rest is scratch.  Calls that may overlap in time (other streams, graphs replayed side
  *               by side) need a workspace each.
+ * Many rows: the tiled kernel, over the cache, or over its values in bf16 if those fit the
+ * workspace and are cheaper to make once (4 bytes each for a pair of K and V: a larger workspace takes longer caches of few heads).
  * The library allocates nothing and keeps nothing: a call may be captured into a graph as it is.
  * A NaN in a row of K that a query sees makes its result NaN; one in a row of V at least the component that holds it.  What a query
  * does not see does not reach it, NaN included.
@@ -442,7 +444,8 @@ int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void* v_cache, 
                        float scale, void* out, void* workspace, int64_t workspace_bytes, void* stream);
 int64_t kvra_chunk_attn_q8_workspace_bytes(void);
 
-/* kvra_chunk_attn_row_splits for kvra_chunk_attn_q8 (slices of 16 or 32 virtual rows; the tiled kernel runs kvra_chunk_attn_plan's plan). */
+/* kvra_chunk_attn_row_splits for kvra_chunk_attn_q8 (slices of 16 or 32 virtual rows; the tiled kernel runs kvra_chunk_attn_plan's
+ * plan), with a workspace of that size. */
 int kvra_chunk_attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
                                   int head_dim, int n_cus, int* splits_out);
 

@@ -332,7 +332,7 @@ extern "C" int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void
   if (chunk_len > kMaxTokens || prefix_len > kMaxTokens) return KVRA_EUNSUPPORTED;
   if (chunk_len * (n_q_heads / n_kv_heads) > (int64_t(1) << 30)) return KVRA_EUNSUPPORTED;
   return kvra::launch_chunk_attn_q8(kvra::Q8Cache{k_cache, v_cache, k_scale, v_scale}, q, prefix_len, chunk_len, n_q_heads,
-                                    n_kv_heads, head_dim, scale, out, workspace, static_cast<hipStream_t>(stream));
+                                    n_kv_heads, head_dim, scale, out, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int kvra_chunk_attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,

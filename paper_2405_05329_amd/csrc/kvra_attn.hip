@@ -1525,15 +1525,35 @@ int rows_splits(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int
 
 namespace {
 
+// The workspace of a call over a cache in 8 bits is the caller's: merge counters, then partial-result slots (of the tiled kernel, or of the
+// one for few rows), then the cache's values in bf16 where they are unpacked.
+constexpr int kQ8Counters = 4096;
+static_assert(kQ8Counters >= kCounterInts, "");
+constexpr int64_t kQ8Workspace = int64_t(128) << 20;
+static_assert(kQ8Workspace >= kQ8Counters * int64_t(4) + kStaticSlots * int64_t(4) * kPartialFloats(128), "");
+
+// Tiled launches over a cache in 8 bits: what it saves, in us, to unpack the cache into the workspace first and read that (0: nothing,
+// or there is no room).  Every workgroup converts every tile it meets, a step of which costs 0.3 to 0.45 us more than the bf16 kernel's; the
+// unpacking is a launch and 6 bytes a pair of values.  Both ways were timed on 166 shapes (8 head layouts, prefixes 0 to 48000, 1 to 2048
+// tokens), and the better one is taken on all but five (7 % lost on the worst).  71 heads x 64 on one, 1088 tokens behind 7104: 192 us
+// converting, 157 unpacked; 32 heads x 128, 1024 behind 1000: 49 and 51.
+float unpacking_saves(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int n_kv_heads, int head_dim, int64_t workspace_bytes) {
+  const int64_t values = (prefix_len + chunk_len) * n_kv_heads * head_dim;       // of K, and of V
+  if (kQ8Counters * int64_t(4) + plan.scratch_slots * attn_partial_bytes(head_dim) + 4 * values > workspace_bytes) return 0.0f;
+  const float steps = static_cast<float>(plan.steps_per_slot), millions = static_cast<float>(values) * 1e-6f;
+  const float full = steps * static_cast<float>(plan.rows_per_tile) / 256.0f;
+  return std::max(0.0f, head_dim == 128 ? 0.34f * steps + 0.02f * full - 2.2f - 0.97f * millions : 0.3f * steps + 0.13f * full - 1.9f - 0.76f * millions);
+}
+
 // The same choice over a cache in 8 bits: rows of a slice of the kernel for few rows and workgroups for each, or *splits = 0.
 // Expected times of both kernels in us, fitted to 299 timed shapes (14 head layouts, prefixes 0 to 128000, 1 to 16000 tokens); the choice
-// costs 0.2 % against choosing by hindsight, 13 % on the worst of them (8 heads x 128 on 2, 192 tokens behind 128000: 154 us tiled,
-// 136 in slices).  256 tokens behind 4000, 32 heads x 128: 45.4 tiled, 27.3 in slices; 1024: 84.2 and 110.4.
+// costs 0.15 % against choosing by hindsight, 13 % on the worst of them (8 heads x 128 on 2, 192 tokens behind 128000: 154 us tiled,
+// 136 in slices).  256 tokens behind 4000, 32 heads x 128: 45.4 tiled, 27.3 in slices; 1024: 84.2 and 110.4.  (Tiled: the better of both ways.)
 //   slices  a launch and its merge, rounds of workgroups (head_dim 64: two to a CU), the steps of a wave with the work spread evenly and as
 //           it falls
 //   tiled   tile steps of the busiest slot, more for full row tiles, and the merging of cut units: all of them, and one unit's pieces
 void rows_q8_shape(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus,
-                   int* rows, int* splits) {
+                   int64_t workspace_bytes, int* rows, int* splits) {
   const int64_t vrows = chunk_len * (n_q_heads / n_kv_heads);
   *rows = vrows <= 16 ? 16 : 32;
   *splits = 0;
@@ -1559,6 +1579,7 @@ void rows_q8_shape(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, 
     sliced = 4.5f + (s > 1 ? 2.9f + 0.28f * static_cast<float>(s) : 0.0f) + 6.25f * (rounds - 1.0f) + 1.54f * load + (rounds > 1.0f ? 0.43f * mean_depth : 0.6f * depth);
     tiled = -2.6f + 1.33f * steps + 0.66f * full + (plan.partial_pieces > 0 ? 6.6f + 9.4f * cut + 0.68f * joined : 0.0f);
   }
+  tiled -= unpacking_saves(plan, prefix_len, chunk_len, n_kv_heads, head_dim, workspace_bytes);
   if (sliced < tiled) *splits = static_cast<int>(s);
 }
 
@@ -1569,7 +1590,7 @@ int attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int
   const int rc = plan_chunk_attn(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, true, &plan);
   if (rc != KVRA_OK) return rc;
   int rows = 0;
-  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, &rows, splits);
+  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, kQ8Workspace, &rows, splits);
   return KVRA_OK;
 }
 
@@ -1640,18 +1661,10 @@ int launch_chunk_attn(const AttnLaunch& l, const void* q, const void* k_cache, c
 }
 
 // ---- over a cache in 8 bits --------------------------------------------------------------------
-// The workspace is the caller's: merge counters, then the partial-result slots (of the tiled kernel, or of the one for few rows).
-namespace {
-
-constexpr int kQ8Counters = 4096;
-static_assert(kQ8Counters >= kCounterInts, "");
-
-}  // namespace
-
-int64_t attn_q8_workspace_bytes() { return (kQ8Counters * int64_t(4) + kStaticSlots * attn_partial_bytes(128) + 4095) / 4096 * 4096; }
+int64_t attn_q8_workspace_bytes() { return kQ8Workspace; }
 
 int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
-                         int head_dim, float scale, void* out, void* workspace, hipStream_t stream) {
+                         int head_dim, float scale, void* out, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
   const int cus = current_device_cus();
   if (cus < 1) return KVRA_ENODEVICE;
   AttnPlan plan;
@@ -1662,7 +1675,7 @@ int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len
   int* const counters = static_cast<int*>(workspace);
   float* const partial = reinterpret_cast<float*>(counters + kQ8Counters);
   int rows = 0, splits = 0;
-  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, &rows, &splits);
+  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, workspace_bytes, &rows, &splits);
   if (splits > 0)
     return launch_attn_rows_q8(cache, q, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, scale, out, rows, splits, partial,
                                counters, stream);
@@ -1678,12 +1691,24 @@ int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len
 #ifdef KVRA_TRACE
   a.trace = nullptr;
 #endif
+  const dim3 grid(static_cast<unsigned>(plan.groups * plan.slots)), block(kThreads);
+  const unsigned rings = 2u * kStages * static_cast<unsigned>(a.bn) * static_cast<unsigned>(head_dim) * 2u;
+  const int64_t values = (prefix_len + chunk_len) * n_kv_heads * head_dim;       // of K, and of V
+  char* const unpacked = reinterpret_cast<char*>(partial) + plan.scratch_slots * attn_partial_bytes(head_dim);
+  if (unpacking_saves(plan, prefix_len, chunk_len, n_kv_heads, head_dim, workspace_bytes) > 0.0f) {
+    rc = launch_unpack_q8(cache, prefix_len + chunk_len, prefix_len + 1, n_kv_heads, head_dim, unpacked, unpacked + 2 * values, stream);
+    if (rc != KVRA_OK) return rc;
+    a.k = reinterpret_cast<const __bf16*>(unpacked);
+    a.v = a.k + values;
+    AttnArgs& same = a;
+    return head_dim == 128 ? launch_kernel(chunk_attn_kernel<128>, grid, block, same, stream, rings)
+                           : launch_kernel(chunk_attn_kernel<64>, grid, block, same, stream, rings);
+  }
   a.k8 = static_cast<const unsigned char*>(cache.k);
   a.v8 = static_cast<const unsigned char*>(cache.v);
   a.k_scale = static_cast<const unsigned char*>(cache.k_scale);
   a.v_scale = static_cast<const unsigned char*>(cache.v_scale);
-  const unsigned smem = 2u * kStages * static_cast<unsigned>(a.bn) * static_cast<unsigned>(head_dim) * 2u + kWaves * 6144u + 128u;   // rings, bytes, marks
-  const dim3 grid(static_cast<unsigned>(plan.groups * plan.slots)), block(kThreads);
+  const unsigned smem = rings + kWaves * 6144u + 128u;   // rings, bytes, marks
   return head_dim == 128 ? launch_kernel(chunk_attn_q8_kernel<128>, grid, block, a, stream, smem)
                          : launch_kernel(chunk_attn_q8_kernel<64>, grid, block, a, stream, smem);
 }

@@ -139,9 +139,11 @@ int launch_attn_rows_q8(const Q8Cache& cache, const void* q, int64_t prefix_len,
                         int head_dim, float scale, void* out, int rows, int splits, float* partial, int* counters,
                         hipStream_t stream);
 int64_t attn_rows_q8_slot_bytes(int head_dim, int rows);
+// Rows [0, rows) of the cache in bf16; rows from hidden_from on are hidden from some query.
+int launch_unpack_q8(const Q8Cache& cache, int64_t rows, int64_t hidden_from, int n_kv_heads, int head_dim, void* k, void* v, hipStream_t stream);
 int64_t attn_q8_workspace_bytes();
 int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
-                         int head_dim, float scale, void* out, void* workspace, hipStream_t stream);
+                         int head_dim, float scale, void* out, void* workspace, int64_t workspace_bytes, hipStream_t stream);
 int attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus, int* splits);
 int current_device_cus();   // 0 if it cannot be asked
 

@@ -188,7 +188,9 @@ def test_attention(H, Hkv, d, prefix, c):
 
 # launches of the kernel with 256 rows a workgroup: whole and cut units, gangs, one and several rounds, row tiles that are not full,
 # more than 64 tile steps, tiles past the end, groups of heads
+# (over the cache: 16 and 32 heads of their own and (8, 8, 128, 20000, 700), but for (32, 32, 128, 0, 4200); the others unpack it)
 TILED = [
+    (16, 16, 128, 20000, 600), (32, 32, 64, 9000, 900),
     (32, 32, 128, 100, 1100), (32, 8, 128, 1000, 1090), (32, 32, 128, 3000, 777), (32, 1, 128, 700, 1301), (16, 16, 128, 12000, 500), (8, 8, 128, 20000, 700),
     (32, 32, 128, 0, 4200), (71, 1, 64, 4096, 600), (71, 1, 64, 100, 1500), (8, 8, 64, 20000, 1500), (8, 8, 64, 0, 6000), (16, 8, 64, 3000, 3000),
 ]
@@ -251,7 +253,7 @@ def test_attention_score_ranges(d, H, Hkv, prefix, c, kind):
 
 
 @pytest.mark.parametrize("H,Hkv,d,prefix,c", [(4, 2, 64, 100, 200), (4, 2, 128, 40, 300), (2, 2, 128, 1000, 70), (71, 1, 64, 64, 66), (4, 2, 128, 200, 1),
-                                              (8, 8, 128, 0, 1500), (16, 1, 64, 0, 900), (32, 32, 128, 100, 1100), (71, 1, 64, 4096, 600)])
+                                              (8, 8, 128, 0, 1500), (16, 1, 64, 0, 900), (32, 32, 128, 100, 1100), (71, 1, 64, 4096, 600), (32, 32, 128, 3000, 777), (32, 32, 64, 9000, 900)])
 def test_attention_nan_reaches_those_that_see_it(H, Hkv, d, prefix, c):
     """NaN in K and in V, in rows of the chunk and of the prefix.  Heads that do not read it keep their bits.  A wave that meets a NaN
     may take its rows' exponents relative to another reference: the rows before it then round otherwise, each result within its bound of
@@ -276,6 +278,24 @@ def test_attention_nan_reaches_those_that_see_it(H, Hkv, d, prefix, c):
             assert np.all(np.abs(f64(got[:r]) - f64(clean[:r])) <= apart[:r])
             seen = f64(got[r:, mine])
             assert np.isnan(seen).all() if which == 0 else np.isnan(seen[..., col]).all()
+
+
+@pytest.mark.parametrize("H,Hkv,d,prefix,c", [(32, 8, 128, 15296, 1088), (8, 8, 64, 40000, 900)])
+def test_attention_with_a_larger_workspace(H, Hkv, d, prefix, c):
+    """Room to unpack a longer cache: another kernel, the same bits."""
+    n = prefix + c
+    q = to_dev(synth.normal_bf16(9, 64, 0, (c, H, d)))
+    caches = [bytes_dev(t) for pair in (random_cache(7, n, n, Hkv, d), random_cache(8, n, n, Hkv, d)) for t in pair]
+    caches = [caches[0], caches[2], caches[1], caches[3]]
+    size, outs = kvra.kvra_chunk_attn_q8_workspace_bytes(), []
+    assert kvra.kvra_chunk_attn_q8_row_splits(prefix, c, H, Hkv, d, torch.cuda.get_device_properties(0).multi_processor_count) == 0
+    for more in (0, 1 << 28):
+        ws = torch.zeros(size + more + 4096, dtype=torch.uint8, device="cuda")
+        ws[size + more:] = 0xA5
+        outs.append(torch.full_like(q, 7.0))
+        kvra.kvra_chunk_attn_q8(q, *caches, prefix, c, H, Hkv, d, 0.09, outs[-1], ws, size + more)
+        assert bool((ws[size + more:] == 0xA5).all()) and not bool(ws[:16384].any())
+    assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
 
 
 def test_attention_on_two_streams_with_a_workspace_each():
