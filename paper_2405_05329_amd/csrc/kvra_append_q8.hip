@@ -1,5 +1,6 @@
 // kvra_append_kv_q8: rotary embedding, and cache population in e4m3 with a power-of-two scale for each block of 64 tokens and
-// head.  HBM-bound: K, V and Q are read once (2 bytes an element), K and V written as bytes.
+// head.  HBM-bound: K, V and Q are read once (2 bytes an element), K and V written as bytes.  5824 tokens of 32 heads x 128: 50 us, 4.8 TB/s
+// (a large copy: 5.2); a token 4.6 us, a launch and two trips to memory.
 //
 // A block's scale needs the largest of its 64 x head_dim values before the first can be written, so a workgroup owns a
 // (block, few heads) pair, holds a head's K and V rows of the block in registers (16 elements of each per thread) and meets
