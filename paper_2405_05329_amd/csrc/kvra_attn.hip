@@ -400,7 +400,7 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
 #pragma unroll
   for (int r = 0; r < 3; ++r) {
     raw_k[r] = uniform(raw_lds + (r + phase + 2) % 3 * 1024);
-    raw_v[r] = uniform(raw_lds + 3072 + (r + phase + 1) % 3 * 1024);
+    raw_v[r] = uniform(raw_lds + 3 * 1024 + (r + phase + 1) % 3 * 1024);
   }
   // Sends for a step's bytes, three steps ahead of it.  Walked tile by tile: offset of the V tile in a cache, rows from it to the end,
   // bytes of those in the tile (a lane beyond gets zeros), which the K tile of one step hands on to the V tile of the next.
@@ -799,7 +799,7 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
     if constexpr (Q8) {
       float kf, vf;
       factors(j, &kf, &vf);
-      const unsigned k_slot = raw_lds + (st + 2) % 3 * 1024, v_slot = raw_lds + 3072 + (st + 1) % 3 * 1024;
+      const unsigned k_slot = raw_lds + (st + 2) % 3 * 1024, v_slot = raw_lds + 3 * 1024 + (st + 1) % 3 * 1024;
       asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
       mark_nan(v_slot, st + 1);
       put_values(raw_at(k_slot), kf, static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsK((st + 2) % kStages))), k_put);

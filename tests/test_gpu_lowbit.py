@@ -298,6 +298,42 @@ def test_attention_with_a_larger_workspace(H, Hkv, d, prefix, c):
     assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
 
 
+@pytest.mark.parametrize("H,Hkv,d,prefix,c", [(71, 1, 64, 4096, 600), (32, 32, 128, 3000, 777), (8, 8, 128, 9000, 1), (8, 2, 128, 1699, 300)])
+def test_attention_in_a_graph(H, Hkv, d, prefix, c):
+    """Each of the ways a call can go (unpacked, tiled, slices shared by workgroups, slices), captured; replays with other queries and
+    caches in the same tensors, with eager calls over the same workspace between them."""
+    n, ws = prefix + c, workspace()
+    q = torch.empty((c, H, d), dtype=torch.bfloat16, device="cuda")
+    caches = [bytes_dev(np.zeros((n, Hkv, d), np.uint8)) for _ in range(2)] + [bytes_dev(np.zeros(((n + 63) // 64, Hkv), np.uint8)) for _ in range(2)]
+
+    def fill(i):
+        q.copy_(to_dev(synth.normal_bf16(9, 70 + i, 0, (c, H, d))))
+        for j in range(2):
+            codes, scales = random_cache(40 + 2 * i + j, n, n, Hkv, d)
+            caches[j].copy_(bytes_dev(codes))
+            caches[2 + j].copy_(bytes_dev(scales))
+
+    def call(out, stream=None):
+        kvra.kvra_chunk_attn_q8(q, *caches, prefix, c, H, Hkv, d, 0.1, out, ws, ws.numel(), stream)
+
+    fill(0)
+    out, eager = torch.empty_like(q), torch.empty_like(q)
+    call(eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, torch.cuda.current_stream())
+    for i in range(4):
+        fill(i)
+        torch.cuda.synchronize()
+        out.fill_(7.0)
+        graph.replay()
+        call(eager, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), eager.view(torch.int16))
+    assert not bool(ws[:16384].any())
+
+
 def test_attention_on_two_streams_with_a_workspace_each():
     H, Hkv, d, prefix, c = 8, 8, 128, 9000, 1
     jobs = []
