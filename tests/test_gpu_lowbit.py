@@ -298,6 +298,41 @@ def test_attention_with_a_larger_workspace(H, Hkv, d, prefix, c):
     assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
 
 
+@pytest.mark.parametrize("c,tiled", [(1, False), (70, False), (700, True)])
+def test_a_cache_beyond_4_gib(c, tiled):
+    """One key of each head, behind the first 2^32 bytes, whose score exceeds all others by 90 or more (n e^-90 < 2^-100: what is left of the
+    others is below bf16's half step of the result): the result is its row of V.  The rows of the chunk come in by an append there."""
+    H, d, prefix = 32, 128, 1_100_000
+    n, dev = prefix + c, "cuda"
+    kc, vc = (torch.zeros((n, H, d), dtype=torch.uint8, device=dev) for _ in range(2))
+    ks, vs = (torch.full(((n + 63) // 64, H), 127, dtype=torch.uint8, device=dev) for _ in range(2))
+    assert (prefix - 40) * H * d > 1 << 32
+    assert (kvra.kvra_chunk_attn_q8_row_splits(prefix, c, H, H, d, torch.cuda.get_device_properties(0).multi_processor_count) == 0) == tiled
+    k = torch.zeros((c, H, d), dtype=torch.bfloat16, device=dev)
+    v = torch.full((c, H, d), -2.0, dtype=torch.bfloat16, device=dev)
+    k[..., 1] = 1.0
+    kvra.kvra_append_kv_q8(k, v, None, None, kc, vc, ks, vs, prefix, c, n, H, H, d, 0.0)
+    torch.cuda.synchronize()
+    # 1 and -2 as the appended rows' codes stand for them, scales of their blocks included
+    first = prefix // 64
+    factor = torch.exp2(torch.stack([ks, vs])[:, first:].double() - 127).repeat_interleave(64, dim=1)[:, prefix - 64 * first:n - 64 * first]
+    assert bool((kc[prefix:, :, 1].view(torch.float8_e4m3fn).double() * factor[0] == 1.0).all())
+    assert bool((vc[prefix:].view(torch.float8_e4m3fn).double() * factor[1][..., None] == -2.0).all())
+    assert not bool(kc[:prefix].any()) and not bool(vc[:prefix].any())
+    key = prefix - 40 - torch.arange(H, device=dev) * 13                  # its own block for many a head, all ahead of the chunk
+    heads = torch.arange(H, device=dev)
+    kc[key, heads, 0] = torch.full((H,), 64.0, device=dev).to(torch.float8_e4m3fn).view(torch.uint8)
+    row = torch.arange(d, device=dev)[None] % 7 + heads[:, None] % 5 + 1.0     # 1 .. 11: exact in e4m3
+    vc[key, heads] = row.to(torch.float8_e4m3fn).view(torch.uint8)
+    ks[key // 64, heads] = 127
+    vs[key // 64, heads] = 127
+    q = torch.zeros((c, H, d), dtype=torch.bfloat16, device=dev)
+    q[..., 0] = 16.0
+    out, ws = torch.empty_like(q), workspace()
+    kvra.kvra_chunk_attn_q8(q, kc, vc, ks, vs, prefix, c, H, H, d, 0.09, out, ws, ws.numel())
+    assert bool((out.float() == row[None]).all())
+
+
 @pytest.mark.parametrize("H,Hkv,d,prefix,c", [(71, 1, 64, 4096, 600), (32, 32, 128, 3000, 777), (8, 8, 128, 9000, 1), (8, 2, 128, 1699, 300)])
 def test_attention_in_a_graph(H, Hkv, d, prefix, c):
     """Each of the ways a call can go (unpacked, tiled, slices shared by workgroups, slices), captured; replays with other queries and
