@@ -399,8 +399,9 @@ int kvra_layer_chunk(const kvra_layer* layer, const void* x, void* y, void* k_ca
  *   weights  e2m1 (0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives), two to a byte, the first of a pair in the low
  *            four bits, a scale for each 32 consecutive values of a row.
  * A block's exponent e is the smallest with which its largest finite magnitude does not overflow (<= 448 * 2^e,
- * <= 6 * 2^e), kept within -100 .. 120; values are rounded to nearest, ties to even.  A value of either format
- * times its scale is an exact bf16 number (e4m3: up to 248 * 2^120): the calls compute with those.
+ * <= 6 * 2^e), kept within -100 .. 120; values are rounded to nearest, ties to even.  Finite values beyond what the exponent 120 holds
+ * become the largest it does: 240 * 2^120 = 3.19e38 in the cache (the next code, 256, would be infinite in bf16), 6 * 2^120 = 8e36 in the
+ * weights.  So what a finite value is stored as, times its scale, is an exact and finite bf16 number: the calls compute with those.
  * Tensors are 16-byte aligned, scales of weights 2-byte (KVRA_EINVAL otherwise).
  */
 
@@ -436,7 +437,7 @@ int kvra_append_kv_q8(const void* k_in, const void* v_in, const void* q_in, void
  * workspace and are cheaper to make once (4 bytes each for a pair of K and V: a larger workspace takes longer caches of few heads).
  * The library allocates nothing and keeps nothing: a call may be captured into a graph as it is.
  * A NaN in a row of K that a query sees makes its result NaN; one in a row of V at least the component that holds it.  What a query
- * does not see does not reach it, NaN included.
+ * does not see does not reach it, NaN included.  Sums over keys are fp32: one beyond 3.4e38 is infinite, whatever the mean of its terms.
  * Errors: KVRA_EINVAL (also: workspace short or misaligned), KVRA_EUNSUPPORTED, KVRA_ELAUNCH, KVRA_ENODEVICE.
  */
 int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,

@@ -2,7 +2,9 @@
 
 Formats: e4m3 (OCP, no infinities) and e2m1 values with a power-of-two scale per block, held as exponent + 127.  A block's
 exponent is the smallest with which its largest finite magnitude stays within the largest value of the format (448, 6), kept in
-[-100, 120]; values are rounded to nearest, ties to the even code.  Pins: tests/test_oracle_lowbit.py."""
+[-100, 120]; values are rounded to nearest, ties to the even code, those beyond the largest code to that.  With the exponent 120 the
+largest code of the cache is 240: the next, 256, would stand for 2^128, which bf16 does not hold.  Pins:
+tests/test_oracle_lowbit.py, tests/test_oracle_lowbit_range.py."""
 import numpy as np
 
 from . import kvra_oracle as orc
@@ -35,8 +37,10 @@ def nearest(x, values):
 
 def e4m3_codes(x, e):
     """x * 2^-e as e4m3 bytes; what is not finite is NaN."""
+    e = np.asarray(e, dtype=np.float64)
+    most = np.where(e >= E_MAX, 240.0, E4M3[-1])
     with np.errstate(invalid="ignore"):
-        code = nearest(np.where(np.isfinite(x), x, 0.0) * 2.0 ** -np.asarray(e, dtype=np.float64), E4M3)
+        code = nearest(np.clip(np.where(np.isfinite(x), x, 0.0) * 2.0 ** -e, -most, most), E4M3)
     return np.where(np.isfinite(x), code, 127 | np.signbit(x) * 128).astype(np.uint8)
 
 

@@ -67,6 +67,18 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a < INFINITY ? a : 0.0f;
 }
 
+// Finite values beyond the cache's largest, to that: a magnitude's bits rise with it.  (Only a block with the largest scale can meet one.)
+__device__ __forceinline__ float within_cache(float x) {
+  const unsigned u = __float_as_uint(x), mag = u & 0x7FFFFFFFu;
+  return mag < 0x7F800000u ? __uint_as_float(min(mag, kCacheMost << 16) | (u & 0x80000000u)) : x;
+}
+
+__device__ __forceinline__ u16x8 within_cache(u16x8 b) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) b[e] = static_cast<unsigned short>(__float_as_uint(within_cache(widen(b[e]))) >> 16);
+  return b;
+}
+
 __device__ __forceinline__ unsigned pack4(float a, float b, float c, float d) {
   unsigned r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
@@ -194,7 +206,7 @@ __global__ __launch_bounds__(4 * D) void append_q8_kernel(AppendQ8Args a) {
   for (int h = h0; h < h1; ++h) {
     const long long row = ((first + t) * a.n_kv_heads + h) * D;
     const long long scale_at = (first / 64) * a.n_kv_heads + h;
-    const u16x8 v0 = now.v0, v1 = now.v1;
+    u16x8 v0 = now.v0, v1 = now.v1;
     float k[16];
     float kmax = 0.0f, vmax = 0.0f;
     const int k_old = now.k_old - 127, v_old = now.v_old - 127;
@@ -259,6 +271,14 @@ __global__ __launch_bounds__(4 * D) void append_q8_kernel(AppendQ8Args a) {
       }
     } else if (fresh) {
       const float kf = power_of_two(-ke), vf = power_of_two(-ve);
+      if (__builtin_expect(ke == kScaleMax, 0)) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) k[e] = within_cache(k[e]);
+      }
+      if (__builtin_expect(ve == kScaleMax, 0)) {
+        v0 = within_cache(v0);
+        v1 = within_cache(v1);
+      }
       *reinterpret_cast<u32x2*>(a.k_cache + row + 8 * j) = pack8(k, kf);
       *reinterpret_cast<u32x2*>(a.k_cache + row + HALF + 8 * j) = pack8(k + 8, kf);
       const u32x2 w0 = pack8(v0, vf), w1 = pack8(v1, vf);

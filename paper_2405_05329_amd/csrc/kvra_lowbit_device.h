@@ -10,6 +10,10 @@ namespace kvra {
 // overflows, kept within bounds that leave every value it can stand for a normal bf16 number.
 constexpr int kScaleMin = -100, kScaleMax = 120;
 
+// The top 16 bits of 240 * 2^kScaleMax (as of every fp32 number above it): the largest finite value of the cache.  The next code with that
+// scale, 256, stands for 2^128, which is infinity in bf16 and would reach even queries that do not see it (a weight of zero times infinity).
+constexpr unsigned kCacheMost = 0x7F70;
+
 // The smallest e with amax <= HIGH * 2^e, HIGH = 448 = 0.875 * 2^9 (e4m3) or 6 = 0.75 * 2^3 (e2m1); amax finite, >= 0.
 template <int HIGH>
 __device__ __forceinline__ int scale_exponent(float amax) {
