@@ -434,7 +434,8 @@ int kvra_append_kv_q8(const void* k_in, const void* v_in, const void* q_in, void
  *               zero; the rest is scratch.  Calls that may overlap in time (other streams, graphs replayed side
  *               by side) need a workspace each.
  * Many rows: the tiled kernel, over the cache, or over its values in bf16 if those fit the
- * workspace and are cheaper to make once (4 bytes each for a pair of K and V: a larger workspace takes longer caches of few heads).
+ * workspace and are cheaper to make once (4 bytes each for a pair of K and V: a larger workspace takes longer caches of few heads; the
+ * result's bits do not depend on its size).
  * The library allocates nothing and keeps nothing: a call may be captured into a graph as it is.
  * A NaN in a row of K that a query sees makes its result NaN; one in a row of V at least the component that holds it.  What a query
  * does not see does not reach it, NaN included.  Sums over keys are fp32: one beyond 3.4e38 is infinite, whatever the mean of its terms.
@@ -446,7 +447,7 @@ int kvra_chunk_attn_q8(const void* q, const void* k_cache, const void* v_cache, 
 int64_t kvra_chunk_attn_q8_workspace_bytes(void);
 
 /* kvra_chunk_attn_row_splits for kvra_chunk_attn_q8 (slices of 16 or 32 virtual rows; the tiled kernel runs kvra_chunk_attn_plan's
- * plan), with a workspace of that size. */
+ * plan), with a workspace of any size. */
 int kvra_chunk_attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads,
                                   int head_dim, int n_cus, int* splits_out);
 

@@ -1554,8 +1554,10 @@ float unpacking_saves(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_le
 //   slices  a launch and its merge, rounds of workgroups (head_dim 64: two to a CU), the steps of a wave with the work spread evenly and as
 //           it falls
 //   tiled   tile steps of the busiest slot, more for full row tiles, and the merging of cut units: all of them, and one unit's pieces
+// The smallest workspace counts, whatever the caller's: slices and tiles round differently, and a result must not depend on spare room.
+// (The two tiled ways give the same bits.  On 40000 shapes a larger one would not have changed the choice.)
 void rows_q8_shape(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int n_q_heads, int n_kv_heads, int head_dim, int cus,
-                   int64_t workspace_bytes, int* rows, int* splits) {
+                   int* rows, int* splits) {
   const int64_t vrows = chunk_len * (n_q_heads / n_kv_heads);
   *rows = vrows <= 16 ? 16 : 32;
   *splits = 0;
@@ -1581,7 +1583,7 @@ void rows_q8_shape(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, 
     sliced = 4.5f + (s > 1 ? 2.9f + 0.28f * static_cast<float>(s) : 0.0f) + 6.25f * (rounds - 1.0f) + 1.54f * load + (rounds > 1.0f ? 0.43f * mean_depth : 0.6f * depth);
     tiled = -2.6f + 1.33f * steps + 0.66f * full + (plan.partial_pieces > 0 ? 6.6f + 9.4f * cut + 0.68f * joined : 0.0f);
   }
-  tiled -= unpacking_saves(plan, prefix_len, chunk_len, n_kv_heads, head_dim, workspace_bytes);
+  tiled -= unpacking_saves(plan, prefix_len, chunk_len, n_kv_heads, head_dim, kQ8Workspace);
   if (sliced < tiled) *splits = static_cast<int>(s);
 }
 
@@ -1592,7 +1594,7 @@ int attn_q8_row_splits(int64_t prefix_len, int64_t chunk_len, int n_q_heads, int
   const int rc = plan_chunk_attn(prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, true, &plan);
   if (rc != KVRA_OK) return rc;
   int rows = 0;
-  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, kQ8Workspace, &rows, splits);
+  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, &rows, splits);
   return KVRA_OK;
 }
 
@@ -1677,7 +1679,7 @@ int launch_chunk_attn_q8(const Q8Cache& cache, const void* q, int64_t prefix_len
   int* const counters = static_cast<int*>(workspace);
   float* const partial = reinterpret_cast<float*>(counters + kQ8Counters);
   int rows = 0, splits = 0;
-  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, workspace_bytes, &rows, &splits);
+  rows_q8_shape(plan, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, cus, &rows, &splits);
   if (splits > 0)
     return launch_attn_rows_q8(cache, q, prefix_len, chunk_len, n_q_heads, n_kv_heads, head_dim, scale, out, rows, splits, partial,
                                counters, stream);

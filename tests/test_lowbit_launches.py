@@ -1,0 +1,47 @@
+"""What the calls over the 8-bit cache and the 4-bit weights enqueue, read off a stand-in for the HIP runtime (lowbit_launches.py): no GPU."""
+import random
+
+import pytest
+
+from lowbit_launches import MIB, append, attn, linear, names, pack, record
+from paper_2405_05329_amd import kvra
+
+
+def _shapes(count):
+    """Caches from a few rows to several times what the smallest workspace holds, one token to thousands."""
+    rng = random.Random(8)
+    out = []
+    while len(out) < count:
+        d, Hkv = rng.choice([64, 128]), rng.choice([1, 2, 3, 5, 8, 16, 32])
+        n, c = int(2.0 ** rng.uniform(4, 19)), int(2.0 ** rng.uniform(0, 12))
+        if c <= n and n * Hkv * d < 1 << 29:
+            out.append((Hkv * rng.choice([1, 2, 4, 8, 32]), Hkv, d, n - c, c))
+    return out
+
+
+def test_slices_or_tiles_is_the_querys_answer_with_any_workspace():
+    """Slices and tiles round differently; spare room in the workspace may only choose between the two tiled ways."""
+    shapes, sizes = _shapes(400), (128 * MIB, 300 * MIB, 1 << 40)
+    results = iter(record([attn(*s, size) for s in shapes for size in sizes]))
+    met = set()
+    for H, Hkv, d, prefix, c in shapes:
+        splits = kvra.kvra_chunk_attn_q8_row_splits(prefix, c, H, Hkv, d, 256)
+        for size in sizes:
+            r = next(results)
+            kernels = names(r)
+            if splits > 0:
+                rows = 16 if c * (H // Hkv) <= 16 else 32
+                assert kernels == [f"attn_rows_q8_kernel<{d}, {rows // 16}>"], (H, Hkv, d, prefix, c, size)
+                assert r["launches"][0]["grid"] == [Hkv, splits, -(-c * (H // Hkv) // rows)]
+            else:
+                assert kernels in ([f"chunk_attn_q8_kernel<{d}>"], [f"unpack_q8_kernel<{d}>", f"chunk_attn_kernel<{d}>"]), (H, Hkv, d, prefix, c, size)
+            met.add((d, kernels[0].split("<")[0]))
+    assert len(met) == 6, met
+
+
+def test_nothing_is_allocated():
+    calls = [attn(*s) for s in _shapes(60)] + [append(32, 8, 128, 100, 1), append(32, 8, 128, 0, 5000), pack(704, 1088)]
+    calls += [linear(m, n, k, form) for m, n, k in ((1, 4096, 4096), (77, 4096, 4096), (777, 4096, 11008), (4096, 4096, 4096))
+              for form in ("plain", "residual", "swiglu")]
+    for call, r in zip(calls, record(calls)):
+        assert r["rc"] == kvra.KVRA_OK and r["launches"] and r["mallocs"] == 0, call
