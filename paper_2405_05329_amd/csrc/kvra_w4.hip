@@ -87,6 +87,14 @@ int launch_unpack_w4(const void* codes, const void* scales, void* w, int64_t n, 
 }
 
 // ---- few tokens --------------------------------------------------------------------------------------------------------
+// Lanes of one wave hand data to each other through LDS.  The hardware carries out a wave's LDS operations in their order, so there is
+// nothing to wait for; this holds the compiler to that order too (to which each lane's own stores and loads are unrelated).
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 struct LinearW4Args {
   const __bf16* x;               // [m, k]
   const unsigned char* w;        // [n, k / 2]
@@ -102,8 +110,7 @@ struct LinearW4Args {
 
 // HBM-bound, and before that bound by the address unit: in the order of the A operand of v_mfma_f32_16x16x32_bf16, 16 neighbouring
 // lanes ask for 16 different rows, 64 lookups an instruction, and the weights came at 2.4 TB/s.  So four neighbouring lanes load
-// 64 bytes of a row, 128 of k, and a buffer of the wave in LDS turns them into operand order (LDS operations of a wave are carried out in
-// order: no barrier); the tokens go the same way, 256 bytes of a row to 16 lanes.  A lane's 16 bytes of codes are one group of one
+// 64 bytes of a row, 128 of k, and a buffer of the wave in LDS turns them into operand order (no workgroup barrier: see wave_exchange); the tokens go the same way, 256 bytes of a row to 16 lanes.  A lane's 16 bytes of codes are one group of one
 // row and feed four products, whose contraction slots are components 32 g + 8 i .. of the 128.  The waves of a workgroup share out k
 // and meet in LDS.  XL: loads of four tokens each.  1 token x 4096 x 4096: 3.7 us (bf16 weights 8.3); 12288 x 4096: 7.1 to 7.7, 3.5 TB/s (19.6);
 // 13 tokens x 11008 x 4096, SwiGLU: 14 us (41.5).  Tried: more chunks ahead in fewer waves: slower.
@@ -190,6 +197,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
 #pragma unroll
         for (int i = 0; i < XL; ++i) b.x[i] = u32x4{0u, 0u, 0u, 0u};
       }
+      wave_exchange();                           // the reads of the chunk before
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) buf[rb * 64 + w_put] = b.w[rb];
 #pragma unroll
@@ -198,6 +206,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
       if (u == 0)
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) next[rb] = load_scales(rb, c + 4);
+      wave_exchange();
       u32x4 w[RB];
       float factor[RB];
 #pragma unroll
