@@ -142,7 +142,8 @@ __global__ __launch_bounds__(64 * WAVES) void linear_w4_rows_kernel(LinearW4Args
   const __amdgpu_buffer_rsrc_t x_res = resource(a.x + static_cast<long long>(tok0) * a.k, static_cast<unsigned>(a.m - tok0) * x_ld);
   const unsigned w_off = static_cast<unsigned>(lane >> 2) * w_ld + 16 * (lane & 3), s_off = static_cast<unsigned>(lane >> 2) * s_ld;
   const unsigned x_off = static_cast<unsigned>(lane >> 4) * x_ld + 16 * (lane & 15);
-  const bool words = (s_ld & 3) == 0;            // a chunk's four scales are a word
+  // a chunk's four scales are a word, at an address that a load of one may have (the tensors are bound to 2 bytes only)
+  const bool words = ((s_ld | static_cast<unsigned>(reinterpret_cast<uintptr_t>(a.ws)) | static_cast<unsigned>(reinterpret_cast<uintptr_t>(a.ws2))) & 3) == 0;
   struct Chunk {
     u32x4 w[RB], x[XL];
   };

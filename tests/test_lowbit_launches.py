@@ -5,6 +5,7 @@ import pytest
 
 from lowbit_launches import MIB, append, attn, linear, names, pack, record
 from paper_2405_05329_amd import kvra
+from test_gpu_lowbit_linear import KERNELS
 
 
 def _shapes(count):
@@ -45,3 +46,13 @@ def test_nothing_is_allocated():
               for form in ("plain", "residual", "swiglu")]
     for call, r in zip(calls, record(calls)):
         assert r["rc"] == kvra.KVRA_OK and r["launches"] and r["mallocs"] == 0, call
+
+
+@pytest.mark.parametrize("m,n,k", KERNELS)
+def test_the_gpu_tests_of_the_4_bit_linear_layer_meet_every_kernel(m, n, k):
+    """Each shape gets the kernel that tests/test_gpu_lowbit_linear.py has it for."""
+    for form, dual, short in (("plain", "false", KERNELS[m, n, k][0]), ("swiglu", "true", KERNELS[m, n, k][1])):
+        kind, args = short[:-1].split("<")
+        want = f"linear_w4_{kind}_kernel<{dual}, {args}{', 8' if kind == 'rows' else ''}>"
+        result, = record([linear(m, n, k, form)])
+        assert names(result) == [want], (form, names(result))
