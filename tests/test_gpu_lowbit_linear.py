@@ -7,7 +7,7 @@ import torch
 from oracle import lowbit
 from paper_2405_05329_amd import kvra, synth
 from gpu_pipeline import to_dev
-from test_gpu_lowbit import bytes_dev, weights
+from test_gpu_lowbit import bytes_dev, f64, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +63,55 @@ def _f64(t):
 
 def _interleaved(pairs, scales):
     return [t for (w, _), s in zip(pairs, scales) for t in (w, s)]
+
+
+def clean(m, n, k, swiglu, seed=6):
+    """Tokens, codes and scales (host), and the result on them."""
+    x = to_dev(synth.normal_bf16(14, m, 5, (m, k)))
+    pairs = [weights(seed + i, n, k) for i in range(1 + swiglu)]
+    ws, ss = [bytes_dev(w) for w, _ in pairs], [s.copy() for _, s in pairs]
+    want = run(x, ws, [bytes_dev(s) for s in ss], m, n, k)
+    assert not bool(torch.isnan(want).any())
+    return x, pairs, ws, ss, want
+
+
+@pytest.mark.parametrize("swiglu", [False, True])
+@pytest.mark.parametrize("m,n,k", KERNELS)
+def test_a_token_of_nan_stays_its_own(m, n, k, swiglu):
+    """Tokens of NaN among the others and behind the last: the others keep their bits (a row that ends inside a stage is followed by
+    the next token)."""
+    x, _, ws, ss, want = clean(m, n, k, swiglu)
+    scales = [bytes_dev(s) for s in ss]
+    behind = torch.full((m + 70, k), float("nan"), dtype=torch.bfloat16, device="cuda")
+    behind[:m] = x
+    assert torch.equal(run(behind[:m], ws, scales, m, n, k), want)
+    bad = torch.arange(m, device="cuda") % 5 == 4
+    behind[:m][bad] = float("nan")
+    got = run(behind[:m], ws, scales, m, n, k)
+    assert bool(torch.isnan(got[bad]).all()) and torch.equal(got[~bad], want[~bad])
+
+
+@pytest.mark.parametrize("swiglu", [False, True])
+@pytest.mark.parametrize("m,n,k", KERNELS)
+def test_a_group_of_nan_stays_in_its_column(m, n, k, swiglu):
+    """In a row's last group, with the next row's data behind it, and in a next row's first group, with a row's end ahead of it."""
+    x, _, ws, ss, want = clean(m, n, k, swiglu)
+    columns = {0: -1, 2: 0, 5: -1, 17: k // 64, n // 2: -1, n // 2 + 3: 0, n - 1: -1, n - 3: 0}
+    hit = torch.zeros(n, dtype=torch.bool, device="cuda")
+    for i, (row, group) in enumerate(columns.items()):
+        ss[i % len(ss)][row, group] = 255
+        hit[row] = True
+    got = run(x, ws, [bytes_dev(s) for s in ss], m, n, k)
+    assert bool(torch.isnan(got[:, hit]).all()) and torch.equal(got[:, ~hit], want[:, ~hit])
+
+
+@pytest.mark.parametrize("m,n,k", KERNELS)
+def test_groups_of_any_magnitude(m, n, k):
+    """Scales from 2^-60 to 2^60 along every row: a scale used one group, one stage or one row off would show."""
+    x = synth.normal_bf16(14, m, 5, (m, k))
+    w, _ = weights(6, n, k)
+    s = np.random.default_rng(32).integers(127 - 60, 127 + 61, (n, k // 32)).astype(np.uint8)
+    rows = [r for r in sorted({0, 1, 15, 16, 63, 64, 127, 128, 1023, 1024, m // 2, m - 1}) if r < m]
+    got = _f64(run(to_dev(x), [bytes_dev(w)], [bytes_dev(s)], m, n, k))[rows]
+    want, terms = lowbit.linear(f64(x[rows]), w, s)
+    assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) * (1 + 2.0 ** -8) + (k / 32 + 48) * 2.0 ** -24 * terms)
