@@ -5,7 +5,10 @@ import pytest
 
 from lowbit_launches import MIB, append, attn, linear, names, pack, record
 from paper_2405_05329_amd import kvra
+from test_gpu_lowbit import TILED
+from test_gpu_lowbit_converting import CUT, SHORT
 from test_gpu_lowbit_linear import KERNELS
+from test_gpu_lowbit_long import SLICES, TILES
 
 
 def _shapes(count):
@@ -56,3 +59,28 @@ def test_the_gpu_tests_of_the_4_bit_linear_layer_meet_every_kernel(m, n, k):
         want = f"linear_w4_{kind}_kernel<{dual}, {args}{', 8' if kind == 'rows' else ''}>"
         result, = record([linear(m, n, k, form)])
         assert names(result) == [want], (form, names(result))
+
+
+@pytest.mark.parametrize("H,Hkv,d,prefix,c", TILES)
+def test_the_gpu_tests_of_long_caches_meet_the_kernels_they_are_for(H, Hkv, d, prefix, c):
+    """More than 64 steps to a piece of the tiled kernel, converting or over the unpacked cache."""
+    result, = record([attn(H, Hkv, d, prefix, c)])
+    assert (names(result)[0] == f"unpack_q8_kernel<{d}>") == TILES[H, Hkv, d, prefix, c]
+    pieces = kvra.kvra_chunk_attn_pieces(prefix, c, H, Hkv, d, 256)
+    assert max(p["jt1"] - p["jt0"] for p in pieces) > 64
+
+
+def test_the_tiled_gpu_tests_meet_both_ways():
+    shapes = TILED + SHORT + CUT
+    for r, s in zip(record([attn(*s) for s in SHORT + CUT]), SHORT + CUT):
+        assert names(r) == [f"chunk_attn_q8_kernel<{s[2]}>"], s
+    for s in CUT:
+        assert kvra.kvra_chunk_attn_plan(s[3], s[4], s[0], s[1], s[2], 256)["partial_pieces"] > 0
+    ways = {d: {names(r)[0] for r in record([attn(*s) for s in shapes if s[2] == d])} for d in (64, 128)}
+    assert ways == {d: {f"unpack_q8_kernel<{d}>", f"chunk_attn_q8_kernel<{d}>"} for d in (64, 128)}
+
+
+def test_the_long_slices_have_more_than_64_tiles_a_wave():
+    for H, Hkv, d, prefix, c in SLICES:
+        splits = kvra.kvra_chunk_attn_q8_row_splits(prefix, c, H, Hkv, d, 256)
+        assert splits > 0 and (prefix + c) // 64 > 64 * 8 * splits, (H, Hkv, d)
