@@ -21,7 +21,8 @@ DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang"
 # The attention kernel lives at the edge of its 256 vector registers: what -O3 adds for it (global value numbering and
 # loop-invariant motion late in the code generator) keeps more addresses alive and ends in 346 spilled vector registers; at
 # -O2 no vector register is spilled (77 scalar ones are at head_dim 128, 58 at 64, to lanes of vector registers and 36 bytes
-# of scratch, outside the tile loop).
+# of scratch, outside the tile loop).  The kernel that converts an 8-bit cache spills 9 vector registers at head_dim 128 and 15 at
+# 64 (104 and 64 bytes of scratch), read back ahead of its tile loop, behind it and where a NaN was met.
 FILE_FLAGS = {"kvra_attn.hip": ["-O2"]}
 
 TRACE_LIB = os.path.join(PKG, "libkvra_trace.so")

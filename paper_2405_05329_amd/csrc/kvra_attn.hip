@@ -323,7 +323,10 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
   const int jw = wave_active ? min(max(wmax / BN + 1 - jt0, 0), nt) : 0;
 
   // Q fragments: B operand of S^T, lane (n, g4) holds Q[row n][32 ks + 8 g4 .. +7], times
-  // scale * log2(e) (rounded to bf16 again)
+  // scale * log2(e), rounded to bf16 again: what leaves the matrix pipe is then the exponent itself, its accumulator starting at minus
+  // the reference.  With Q as it came the scale would be a multiplication a score, 32 (head_dim 128) or 64 a lane and tile step, in the block
+  // that the matrix pipe waits for.  Error of the result against 64 bits (relative 2-norm, N(0, 1) inputs): 2.9e-3; the kernel for few
+  // rows over the 8-bit cache, which leaves Q alone, 2.3e-3; rounding the exact result to bf16 1.7e-3.
   bf16x8 qf[KS][QB];
   int qpos[QB];
 #pragma unroll
@@ -381,7 +384,7 @@ __device__ __forceinline__ void attend(const Args& a, u32x4* smem, int* last_fla
 
   // ---- Q8 ------------------------------------------------------------------------------------
   // raw: [wave][K, V][tile mod 3] 1 KiB, behind the rings; then a word for each 32 keys of the up to 8 tiles that hold a key hidden
-  // from a row of the workgroup, in which a row of V with a NaN is marked (see stage_v)
+  // from a row of the workgroup, in which a row of V with a NaN is marked (see without_nan)
   constexpr int RAW_CPR = D / 16;
   [[maybe_unused]] const unsigned raw_lds = static_cast<unsigned>(reinterpret_cast<uintptr_t>((lds_void*)ldsV(kStages))) + wave * 6144;
   [[maybe_unused]] unsigned* const bad_rows = reinterpret_cast<unsigned*>(ldsV(kStages)) + kWaves * 1536;
@@ -1537,8 +1540,8 @@ static_assert(kQ8Workspace >= kQ8Counters * int64_t(4) + kStaticSlots * int64_t(
 // Tiled launches over a cache in 8 bits: what it saves, in us, to unpack the cache into the workspace first and read that (0: nothing,
 // or there is no room).  Every workgroup converts every tile it meets, a step of which costs 0.3 to 0.45 us more than the bf16 kernel's; the
 // unpacking is a launch and 6 bytes a pair of values.  Both ways were timed on 166 shapes (8 head layouts, prefixes 0 to 48000, 1 to 2048
-// tokens), and the better one is taken on all but five (7 % lost on the worst).  71 heads x 64 on one, 1088 tokens behind 7104: 192 us
-// converting, 157 unpacked; 32 heads x 128, 1024 behind 1000: 49 and 51.
+// tokens), and the better one is taken on all but five (7 % lost on the worst).  71 heads x 64 on one, 1088 tokens behind 7104: 190 us
+// converting, 158 unpacked; 32 heads x 128, 1024 behind 1000: 49 and 51.
 float unpacking_saves(const AttnPlan& plan, int64_t prefix_len, int64_t chunk_len, int n_kv_heads, int head_dim, int64_t workspace_bytes) {
   const int64_t values = (prefix_len + chunk_len) * n_kv_heads * head_dim;       // of K, and of V
   if (kQ8Counters * int64_t(4) + plan.scratch_slots * attn_partial_bytes(head_dim) + 4 * values > workspace_bytes) return 0.0f;

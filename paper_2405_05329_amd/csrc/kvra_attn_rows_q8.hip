@@ -10,14 +10,15 @@
 // LDS traffic and half the bytes in flight of bf16 tiles; the conversions, 128 a tile and wave at head_dim 128, overlap with the loads.)
 // A slice is 16 rows where a head has no more - a token with up to 16 heads in a group - else 32.
 //
-// us on one MI355X, and those of the bf16 kernel over twice the bytes: 1 token behind 16383, 32 heads x 128: 33 (4.0 TB/s; the same loads
-// alone 27) and 54; 32 heads on 8: 14 and 25; 77 behind 5824, 32 on 8: 20 and 25; 160 tokens, 2 heads x 64: 5.0 and 5.1.  Of a short
+// us on one MI355X, and those of the bf16 kernel over twice the bytes: 1 token behind 16383, 32 heads x 128: 33.6 over four caches in turn
+// (4.0 TB/s; the same loads alone 27.7; as 256 heads behind 2047, without a merge, 29.5) and 54; 32 heads on 8: 14 and 25; 77 behind 5824, 32 on 8: 20 and 25; 160 tokens, 2 heads x 64: 5.0 and 5.1.  Of a short
 // launch half is start, first trip to memory and merge.
 // Tried: K straight to the fp8 matrix instruction, Q in two e4m3 parts that add up to it: half the conversions, the same loop times, and
 // 1 us more ahead of the first tile (77 tokens 23 us).
 //
 // Roundings: Q is used as it came (the softmax scale goes onto the fp32 scores), P is rounded to bf16 for the product with V,
-// the row sums add the unrounded fp32 weights.  Against fp64 that is sqrt(2) times the error of rounding the output alone.
+// the row sums add the unrounded fp32 weights.  P is rounded because it is an operand of the bf16 matrix instruction: in two bf16 parts it would
+// take twice the products with V.  Against fp64 that is sqrt(2) times the error of rounding the output alone (2.3e-3 and 1.7e-3, relative 2-norm).
 #include "kvra_attn_device.h"
 #include "kvra_lowbit_device.h"
 

@@ -540,7 +540,8 @@ int launch_tile(LinearW4Args& a, hipStream_t stream) {
 // Which kernel.  Both take about k times a constant per round of workgroups on the chip's 256 CUs, whatever the round holds: the
 // one for few tokens, 32 rows (SwiGLU 16) x 64 tokens a workgroup, 2.45 us per 1000 of k; the other, 256 rows (128) x 64 tokens, 7.0 us
 // with two groups of waves along k and one workgroup a CU, 12.5 us with one group and two workgroups a CU.  Timed on 100 shapes, n 1024 to
-// 12288, k 1024 to 11008, 40 to 1500 tokens; 4096 x 4096: 128 tokens 13.2 us here, 31.3 there; 512 tokens 43.4 and 32.4.
+// 12288, k 1024 to 11008, 40 to 1500 tokens; 4096 x 4096 (in a graph): 128 tokens 12.1 us here, 30.9 there; 300 tokens 29.8 and 31.0; 512 tokens
+// 40.1 and 32.0.
 template <bool DUAL>
 int launch_any(LinearW4Args& a, hipStream_t stream) {
   const int64_t token_tiles = (a.m + 63) / 64, tiles = token_tiles * ((a.n + (DUAL ? 127 : 255)) / (DUAL ? 128 : 256));
